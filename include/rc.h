@@ -394,6 +394,97 @@ rc_status rc_pool_evict(int64_t P, uint8_t* pool_live, const int32_t* refcount, 
                         const int32_t* match_idx, int64_t Q, int64_t extra_wanted,
                         int32_t* n_free, int32_t* n_evicted, void* hip_stream);
 
+/*
+ * ---- The KV cache held in 4 bits ------------------------------------------------------------------------------------------
+ *
+ * A paged cache whose K and V are e2m1 codes (sign, two exponent bits, one fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), every 32
+ * consecutive dims of a token's head (a group) under one power of two: 4.25 bits a value instead of 16.  rc_cache_write
+ * quantises the tokens of a step into it, rc_cache_attend is the attention that reads it through the block tables (which
+ * rc_remap_block_table rewrites: a shared block is read where its keeper lies), rc_cache_read turns blocks back into the KV
+ * layout that rc_block_norms, the searches and rc_pool_admit take.
+ *
+ * A group's power is the smallest 2^x with (largest magnitude) <= 7 * 2^x, x within -23 .. 13 for fp16 and -125 .. 125 for bf16,
+ * so that every value code * 2^x is a number of the type, exactly; an element goes to the nearest code, halfway to the even one.
+ * An element is off by at most half the step of its code (2^(x-2) at a code of 2 or less, 2^x beyond 4), except that fp16 magnitudes above
+ * 57344 are held as 49152 and bf16 ones above 7 * 2^125 as 6 * 2^125.  A group with an infinity or a NaN in it reads as
+ * NaN throughout.  Powers are held as bytes x + 127 (255: NaN).  A cache serves the type that it was written with.
+ *
+ * Memory: block b of layer l starts at  l*layer_stride + b*rc_cache_block_bytes()  bytes and holds, head by head, T/16 records
+ * of 2176 bytes, each the K and V of 16 tokens:
+ *   0 .. 1023     K codes: group g, token t at (g*16 + t)*16, the group's 32 dims in order, even ones in the low half bytes
+ *   1024 .. 2047  V codes: tokens 4q + r, dims 8i .. 8i+7 at ((q*16 + i)*4 + r)*4, likewise
+ *   2048 .. 2111  K powers: g*16 + t
+ *   2112 .. 2175  V powers: (q*4 + g)*4 + r
+ */
+typedef struct {
+  int32_t n_layers;     /* L                                                                    */
+  int32_t block_tokens; /* T, 16 or 32                                                          */
+  int32_t n_kv_heads;   /* H, 1 .. 16                                                           */
+  int32_t head_dim;     /* 128                                                                  */
+  int32_t dtype;        /* rc_dtype of the values that go in and come out, and of queries       */
+  int64_t n_blocks;     /* blocks of a layer; n_blocks * T < 2^31                               */
+  int64_t layer_stride; /* BYTES between layer l and l+1, a multiple of 16                      */
+} rc_cache_desc;
+
+/* Bytes of a block of one layer, H * T/16 * 2176 (0 on an unsupported shape). */
+size_t rc_cache_block_bytes(int32_t block_tokens, int32_t n_kv_heads, int32_t head_dim);
+
+/*
+ * New tokens into their slots: K and V of n_tokens tokens of every layer are quantised and stored.
+ *
+ *   k, v            DEVICE, element (l, n, h, d) at l*kv_layer_stride + n*token_stride + h*128 + d: slices of a fused projection's
+ *                   output do.  Strides in elements, multiples of 8; pointers 16-byte aligned.
+ *   slots           DEVICE int32 [n_tokens], the same for all layers: block * T + (place in the block).  A token whose slot lies
+ *                   outside [0, n_blocks * T) is not stored (-1: a batch's empty place).  Slots must be distinct.
+ *   cache           DEVICE, 16-byte aligned, updated in place; bytes of other slots stay as they are
+ */
+rc_status rc_cache_write(const rc_cache_desc* desc, const void* k, const void* v, int64_t n_tokens,
+                         int64_t token_stride, int64_t kv_layer_stride, const int32_t* slots, void* cache,
+                         void* hip_stream);
+
+/*
+ * Blocks back out of the cache, in the KV layout of this header (kvdesc: the same L, T, H, head_dim and dtype).
+ *
+ *   ids             DEVICE int32 [n], the same for all layers; a block outside [0, n_blocks) is read as zeros
+ *   k, v            DEVICE, n blocks per layer, 16-byte aligned
+ * The values are exact: no rounding happens on the way out.
+ */
+rc_status rc_cache_read(const rc_cache_desc* desc, const void* cache, const int32_t* ids, int64_t n,
+                        const rc_kv_desc* kvdesc, void* k, void* v, void* hip_stream);
+
+/* Bytes of DEVICE workspace rc_cache_attend needs (0 on bad arguments; up to 71 MB).  It depends on the arguments only and never falls
+ * as R, E, max_q or the layers grow. */
+size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int64_t R, int64_t E, int32_t n_heads, int64_t max_q);
+
+/*
+ * Attention of a step's query tokens over the cached tokens of their requests, causal, every layer an independent problem:
+ *
+ *     out = sum_t p_t v_t,   p = softmax_t(scale * q.k_t),   lse = log sum_t exp(scale * q.k_t)
+ *
+ * Request r has ctx_len[r] tokens in the cache (this step's own among them: rc_cache_write comes first) and the query tokens
+ * q_start[r] .. q_start[r+1] - 1, its last ones: with m of them, query token j stands at position ctx_len[r] - m + j and sees the
+ * positions up to its own, with a window the last `window` of these.  Position t is place t % T of block tables[l][r][t / T];
+ * positions behind the table's end and those of entries outside [0, n_blocks) (-1: no block) are seen by nobody.
+ * n_heads = g * H: query heads h*g .. h*g + g-1 share KV head h.  A query that sees nothing gets 0 and an lse of -inf.
+ *
+ *   tables          DEVICE int32 [L][R][E];  ctx_len: DEVICE int32 [R]
+ *   q_start         DEVICE int32 [R+1], ascending, q_start[R] <= n_q; NULL: one query token per request, in order (n_q >= R, max_q 1)
+ *   q               DEVICE, element (l, n, head, d) at l*q_layer_stride + n*q_token_stride + head*128 + d; strides in
+ *                   elements, multiples of 8; 16-byte aligned
+ *   max_q           HOST, at least the largest number of query tokens of a request (further ones are not computed)
+ *   window          0: none
+ *   out             DEVICE, [L][n_q][n_heads][128] in the cache's dtype, 16-byte aligned;  lse: DEVICE float [L][n_q][n_heads] or NULL.
+ *                   Query tokens that belong to no request keep what out and lse held.
+ *   workspace       DEVICE, 16-byte aligned, rc_cache_attend_workspace_size() bytes.  Contents are scratch.  Calls that share it
+ *                   must not overlap.
+ * Sums and softmax statistics are fp32; the probabilities are rounded to the 16-bit type for the matrix cores.  No atomics: the
+ * same bits on every run.
+ */
+rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const int32_t* tables, int64_t R, int64_t E,
+                          const int32_t* ctx_len, const int32_t* q_start, const void* q, int64_t n_q, int32_t n_heads,
+                          int64_t q_token_stride, int64_t q_layer_stride, int64_t max_q, float scale, int64_t window,
+                          void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* HOST string describing the calling thread's last error ("" if none). Never NULL. */
 const char* rc_last_error(void);
 

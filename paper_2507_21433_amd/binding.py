@@ -21,6 +21,7 @@ EXPORTS = ("rc_block_norms", "rc_match_workspace_size", "rc_match_blocks", "rc_r
            "rc_remap_block_table", "rc_remap_static_scratch_size", "rc_remap_block_table_static", "rc_score_candidates", "rc_layer_mean_workspace_size", "rc_match_blocks_layer_mean",
            "rc_pat_workspace_size", "rc_pat_threshold", "rc_apply_threshold", "rc_pool_admit_workspace_size", "rc_pool_admit",
            "rc_candidate_distances_workspace_size", "rc_candidate_distances", "rc_pool_touch", "rc_refcount_release", "rc_pool_evict",
+           "rc_cache_block_bytes", "rc_cache_write", "rc_cache_read", "rc_cache_attend_workspace_size", "rc_cache_attend",
            "rc_last_error", "rc_version")
 
 
@@ -33,6 +34,11 @@ class RcError(RuntimeError):
 class KvDesc(ctypes.Structure):
     _fields_ = [("n_layers", ctypes.c_int32), ("block_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("layer_stride", ctypes.c_int64)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("block_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_blocks", ctypes.c_int64), ("layer_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -92,6 +98,17 @@ def lib():
         L.rc_refcount_release.restype = i32
         L.rc_pool_evict.argtypes = [i64, vp, vp, vp, vp, i64, i64, vp, vp, vp]
         L.rc_pool_evict.restype = i32
+        cp = ctypes.POINTER(CacheDesc)
+        L.rc_cache_block_bytes.argtypes = [i32, i32, i32]
+        L.rc_cache_block_bytes.restype = sz
+        L.rc_cache_write.argtypes = [cp, vp, vp, i64, i64, i64, vp, vp, vp]
+        L.rc_cache_write.restype = i32
+        L.rc_cache_read.argtypes = [cp, vp, vp, i64, dp, vp, vp, vp]
+        L.rc_cache_read.restype = i32
+        L.rc_cache_attend_workspace_size.argtypes = [cp, i64, i64, i32, i64]
+        L.rc_cache_attend_workspace_size.restype = sz
+        L.rc_cache_attend.argtypes = [cp, vp, vp, i64, i64, vp, vp, vp, i64, i32, i64, i64, i64, f32, i64, vp, vp, vp, sz, vp]
+        L.rc_cache_attend.restype = i32
         L.rc_last_error.restype = ctypes.c_char_p
         L.rc_version.restype = i32
         _lib = L
@@ -415,3 +432,98 @@ def rc_pool_evict(pool_live, refcount, last_used, match_idx, extra_wanted=0, out
     _check(lib().rc_pool_evict(P, _ptr(pool_live), _ptr(refcount), _ptr(last_used), _ptr(match_idx), match_idx.numel(),
                                int(extra_wanted), _ptr(out["n_free"]), _ptr(out["n_evicted"]), _stream()))
     return out
+
+
+RECORD_BYTES = 2176     # 16 tokens' K and V of one head in a 4-bit cache
+
+
+def cache_tensor(n_layers, n_blocks, block_tokens, n_kv_heads, device="cuda"):
+    """An empty 4-bit cache, uint8 [L][n_blocks][H][T/16][2176]: every value of it is 0."""
+    return torch.zeros((n_layers, n_blocks, n_kv_heads, block_tokens // 16, RECORD_BYTES), dtype=torch.uint8, device=device)
+
+
+_cdesc = functools.lru_cache(maxsize=64)(CacheDesc)
+
+
+def _cache_desc(cache, dtype_code):
+    """Descriptor of a cache tensor whose layers are contiguous (the layers themselves may lie apart: some of a larger cache's)."""
+    assert cache.dtype == torch.uint8 and cache.dim() == 5 and cache.shape[4] == RECORD_BYTES, "a cache is uint8 [L][n][H][T/16][2176]"
+    L, n, H, tiles, _ = cache.shape
+    s, block = cache.stride(), H * tiles * RECORD_BYTES
+    assert s[4] == 1 and s[3] == RECORD_BYTES and s[2] == tiles * RECORD_BYTES and (n < 2 or s[1] == block), "a layer of a cache is contiguous"
+    return _cdesc(L, tiles * 16, H, 128, dtype_code, n, s[0] if L > 1 else n * block)
+
+
+def _rows(t):
+    """(token stride, layer stride) of a tensor [L][N][heads][128] whose tokens' heads are contiguous."""
+    L, N, heads, D = t.shape
+    s = t.stride()
+    assert D == 128 and s[3] == 1 and (heads < 2 or s[2] == 128), "the heads of a token are contiguous"
+    token = s[1] if N > 1 else heads * 128
+    return token, s[0] if L > 1 else N * token
+
+
+def rc_cache_write(k, v, slots, cache):
+    """K and V of new tokens [L][N][H][128] into their slots (block * T + place; int32 [N]) of a 4-bit cache, in place."""
+    _dev(k, v, slots, cache)
+    assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype, "K and V of one type and shape, [L][N][H][128]"
+    L, N, H, _ = k.shape
+    assert cache.shape[0] == L and cache.shape[2] == H, "K's layers and heads are the cache's"
+    strides = _rows(k)
+    assert v.stride() == k.stride() or _rows(v) == strides, "K and V of the same strides"
+    assert slots.dtype == torch.int32 and slots.shape == (N,) and slots.is_contiguous()
+    d = _cache_desc(cache, _dtype_code(k))
+    _check(lib().rc_cache_write(ctypes.byref(d), _ptr(k), _ptr(v), N, *strides, _ptr(slots), _ptr(cache), _stream()))
+    return cache
+
+
+def rc_cache_read(cache, ids, dtype=None, k=None, v=None):
+    """The listed blocks (int32 [n]) of a 4-bit cache, exactly: returns (k, v) [L][n][T][H][128], new ones of `dtype` or the given ones."""
+    _dev(cache, ids, k, v)
+    assert ids.dtype == torch.int32 and ids.dim() == 1 and ids.is_contiguous()
+    L, _, H, tiles, _ = cache.shape
+    shape = (L, ids.numel(), tiles * 16, H, 128)
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=cache.device)
+    if v is None:
+        v = torch.empty_like(k)
+    assert k.shape == shape
+    _, kd = _kv_pair(k, v, alike=True)
+    d = _cache_desc(cache, kd.dtype)
+    _check(lib().rc_cache_read(ctypes.byref(d), _ptr(cache), _ptr(ids), ids.numel(), ctypes.byref(kd), _ptr(k), _ptr(v), _stream()))
+    return k, v
+
+
+def rc_cache_attend_workspace_size(cache, dtype, R, E, n_heads, max_q=1):
+    d = _cache_desc(cache, RC_F16 if dtype == torch.float16 else RC_BF16)
+    return lib().rc_cache_attend_workspace_size(ctypes.byref(d), R, E, n_heads, max_q)
+
+
+def rc_cache_attend(q, cache, tables, ctx_len, q_start=None, max_q=1, scale=None, window=0, want_lse=True, workspace=None, out=None,
+                    lse=None):
+    """Causal attention of query tokens [L][N][heads][128] over a 4-bit cache through tables [L][R][E] (int32).
+
+    ctx_len int32 [R]: cached tokens, this step's among them; q_start int32 [R+1]: a request's query tokens (None: one each);
+    max_q: most query tokens of a request.  Returns dict(out [L][N][heads][128], lse float32 [L][N][heads] or None)."""
+    _dev(q, cache, tables, ctx_len, q_start, workspace, out, lse)
+    assert q.dim() == 4 and tables.dim() == 3 and tables.dtype == torch.int32 and tables.is_contiguous()
+    L, N, heads, _ = q.shape
+    _, R, E = tables.shape
+    assert cache.shape[0] == L and tables.shape[0] == L, "the queries' layers are the cache's and the tables'"
+    assert ctx_len.dtype == torch.int32 and ctx_len.shape == (R,) and ctx_len.is_contiguous()
+    if q_start is not None:
+        assert q_start.dtype == torch.int32 and q_start.shape == (R + 1,) and q_start.is_contiguous()
+    d = _cache_desc(cache, _dtype_code(q))
+    if workspace is None:
+        workspace = torch.empty(max(16, lib().rc_cache_attend_workspace_size(ctypes.byref(d), R, E, heads, max_q)), dtype=torch.uint8,
+                                device=q.device)
+    if out is None:
+        out = torch.empty((L, N, heads, 128), dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((L, N, heads), dtype=torch.float32, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
+    assert lse is None or (lse.shape == (L, N, heads) and lse.dtype == torch.float32 and lse.is_contiguous())
+    _check(lib().rc_cache_attend(ctypes.byref(d), _ptr(cache), _ptr(tables), R, E, _ptr(ctx_len), _ptr(q_start), _ptr(q), N, heads,
+                                 *_rows(q), max_q, 128 ** -0.5 if scale is None else float(scale), int(window), _ptr(out), _ptr(lse),
+                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+    return dict(out=out, lse=lse)

@@ -1,0 +1,851 @@
+// rc_cache_attend: softmax attention over the 4-bit paged cache, one pass over the data with a running reference of the softmax.
+//
+// Scores are taken as S^T = K Q^T and outputs as O^T = V^T P^T on 16x16x32 matrix instructions: a row (a query token and head) is a
+// column of both, so that its scores, its probabilities and its sums lie in the same four lanes and the probabilities go from
+// one product into the next as they are.  K and V come from memory as codes in operand order (rc_cache.hpp); a wave turns 16 bytes
+// of codes into 32 operand values with 16 conversions, V with 16 byte permutes more, which pair neighbouring tokens.
+//
+// The softmax's reference is not the running maximum but a number at most 15 below it (in powers of two) and 7 below it when it is
+// set: probabilities stay below 2^15, as fp16 holds them, and the sums are rescaled only where a score passes the reference by 15.
+#include <hip/hip_runtime.h>
+
+#include "rc_attend_plan.hpp"
+#include "rc_cache.hpp"
+
+namespace rc {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr float kNothing = -3e38f;  // the reference of a row that has seen nothing; -infinity would make NaNs of differences
+constexpr float kRoom = 15.f, kBelow = 7.f;
+
+struct AttendArgs {
+  AttendShape s;
+  const char* cache;
+  const int32_t *tables, *ctx_len, *q_start;
+  const char* q;
+  char* out;
+  float* lse;
+  int64_t cache_layer_stride, q_token_stride_b, q_layer_stride_b, n_blocks;
+  float c;  // scale * log2(e)
+  int64_t* before;  // units before each request, [R + 1]; NULL where nothing is joined
+  char* parts;
+};
+
+template <bool BF16>
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Two fp32 numbers rounded to the nearest 16-bit ones.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (BF16)
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+  else
+    return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+}
+template <bool BF16>
+__device__ __forceinline__ float low16(uint32_t w) {
+  if constexpr (BF16)
+    return __uint_as_float(w << 16);
+  else
+    return (float)__builtin_bit_cast(f16x2, w)[0];
+}
+template <bool BF16>
+__device__ __forceinline__ float high16(uint32_t w) {
+  if constexpr (BF16)
+    return __uint_as_float(w & 0xffff0000u);
+  else
+    return (float)__builtin_bit_cast(f16x2, w)[1];
+}
+
+// Over the four lanes l, l + 16, l + 32, l + 48 that hold a row.
+__device__ __forceinline__ float row_max(float x) {
+  u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+  y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
+__device__ __forceinline__ AttendRequest request(const AttendArgs& a, int r) {
+  return a.q_start ? attend_request(a.s, a.ctx_len[r], a.q_start[r], a.q_start[r + 1]) : attend_request(a.s, a.ctx_len[r], r, r + 1);
+}
+
+// ---- Where a workgroup's stretch of the line of units begins, and the walk along it.
+
+struct FindLds {
+  int64_t sums[kWaves], offset;
+  int32_t request;
+};
+
+struct Walk {
+  int64_t at, end, begin;  // units of the line
+  int64_t l;
+  int r, h, t, u;  // layer, request, head, row tile, unit of the item
+  AttendRequest q;
+  AttendItem item;
+};
+
+// Sum of x over the threads up to and including this one; `all` gets the sum over the workgroup.
+__device__ inline int64_t block_scan(int64_t x, FindLds& lds, int64_t& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) lds.sums[wave] = x;
+  __syncthreads();
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) x += lds.sums[w];
+    all += lds.sums[w];
+  }
+  return x;
+}
+
+// Every workgroup counts the units of all requests by itself: for 64 requests two loads and a scan, where a launch of its own
+// would cost more than that.
+__device__ inline bool find(const AttendArgs& a, FindLds& lds, int64_t wg, Walk& w) {
+  int64_t mine = 0, upto = 0, total = 0, all;
+  for (int64_t base = 0; base < a.s.R; base += kThreads) {
+    const int64_t r = base + threadIdx.x;
+    mine = r < a.s.R ? attend_units(a.s, request(a, (int)r)) * a.s.H : 0;
+    upto = block_scan(mine, lds, all) + total;
+    if (wg == 0 && a.before && r < a.s.R) a.before[r] = upto - mine;
+    total += all;
+  }
+  if (wg == 0 && a.before && threadIdx.x == 0) a.before[a.s.R] = total;
+  const int64_t line = total * a.s.L, share = attend_share(a.s, line);
+  w.begin = w.at = wg * share;
+  w.end = w.at + share < line ? w.at + share : line;
+  if (w.at >= w.end) return false;
+  w.l = w.at / total;
+  const int64_t off = w.at - w.l * total;
+  if (a.s.R > kThreads) total = 0;
+  for (int64_t base = 0; base < a.s.R; base += kThreads) {
+    const int64_t r = base + threadIdx.x;
+    if (a.s.R > kThreads) {
+      mine = r < a.s.R ? attend_units(a.s, request(a, (int)r)) * a.s.H : 0;
+      upto = block_scan(mine, lds, all) + total;
+      total += all;
+    }
+    if (off >= upto - mine && off < upto) {
+      lds.request = (int32_t)r;
+      lds.offset = off - (upto - mine);
+    }
+  }
+  __syncthreads();
+  w.r = uniform(lds.request);
+  int64_t rest = uniform(lds.offset);
+  w.q = request(a, w.r);
+  const int64_t units = attend_units(a.s, w.q);
+  w.h = (int)(rest / units);
+  rest -= w.h * units;
+  for (w.t = 0;; ++w.t) {
+    w.item = attend_item(a.s, w.q, w.t);
+    if (rest < w.item.units) break;
+    rest -= w.item.units;
+  }
+  w.u = (int)rest;
+  return true;
+}
+
+// To the next item of a stretch that goes on: only called where there is one.
+__device__ inline void next_item(const AttendArgs& a, Walk& w) {
+  w.u = 0;
+  if (++w.t == w.q.tiles) {
+    w.t = 0;
+    if (++w.h == a.s.H) {
+      w.h = 0;
+      do {
+        if (++w.r == a.s.R) w.r = 0, ++w.l;
+        w.q = request(a, w.r);
+      } while (w.q.tiles == 0);
+    }
+  }
+  w.item = attend_item(a.s, w.q, w.t);
+}
+
+// ---- Loads.
+
+// What a wave holds of 16 tokens: codes in operand order, exponent bytes (K: the lane's token and group; V: four tokens of its group).
+struct Tile {
+  u32x4 k, v;
+  uint32_t ke, ve;
+};
+
+__device__ __forceinline__ void load_tile(Tile& x, const char* rec, int lane) {
+  x.k = *(const u32x4*)(rec + lane * 16);
+  x.v = *(const u32x4*)(rec + kRecordV + lane * 16);
+  x.ke = *(const uint8_t*)(rec + kRecordKExp + lane);
+  x.ve = *(const uint32_t*)(rec + kRecordVExp + ((lane >> 4) * 4 + ((lane & 15) >> 2)) * 4);
+}
+
+// The record of the 16 tokens at position 16 * tile (wave-uniform); block 0's where there is no such block (`there` false): its
+// values are replaced or masked.
+__device__ __forceinline__ const char* record(const AttendArgs& a, const int32_t* table, const char* layer, int h, int tile, bool& there) {
+  const int tiles = a.s.T >> 4, e = a.s.T == 32 ? tile >> 1 : tile;
+  const int id = e < a.s.E ? table[e] : -1;
+  there = id >= 0 && id < a.n_blocks;
+  return layer + (((int64_t)(there ? id : 0) * a.s.H + h) * tiles + (a.s.T == 32 ? tile & 1 : 0)) * kRecordBytes;
+}
+
+// V's exponent bytes with those of tokens that no row sees replaced by that of 1: whatever lies there (memory that was never
+// written) gets a probability of 0, and 0 times infinity or NaN would not be 0.  Token r of the word stands at pos + r.
+__device__ __forceinline__ uint32_t seen_only(uint32_t ve, int pos, bool there, const AttendItem& it) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const bool seen = there && pos + r >= it.low_min && pos + r < it.high_max;
+    const uint32_t m = 0xffu << (8 * r);
+    if (!seen) ve = (ve & ~m) | ((uint32_t)kOneByte << (8 * r));
+  }
+  return ve;
+}
+// ... and those of NaN groups: where only some rows see a token, its NaNs are added to these (poison()).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t ve) {
+  uint32_t f = 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if ((ve >> (8 * r) & 255) == kNanByte) f |= 1u << r;
+  return f;
+}
+__device__ __forceinline__ uint32_t without_nans(uint32_t ve, uint32_t flags) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (flags >> r & 1) ve = (ve & ~(0xffu << (8 * r))) | ((uint32_t)kOneByte << (8 * r));
+  return ve;
+}
+// Two tokens' bits (b, b + 1 of f) as 16-bit ones and zeros.
+template <bool BF16>
+__device__ __forceinline__ uint32_t ones(uint32_t f, int b) {
+  constexpr uint32_t one = BF16 ? 0x3f80u : 0x3c00u;
+  return (f >> b & 1 ? one : 0) | (f >> (b + 1) & 1 ? one << 16 : 0);
+}
+// NaNs of 32 tokens (flags: bit 4 * tile + r, for the lane's group) into the sums of the rows that see them (seen: the same bits for the lane's row): the number
+// of such tokens by row and lane of V's operand, whose 8 dims lie in the 8 sums of that place.
+template <bool BF16>
+__device__ inline void poison(f32x4 (&o)[8], uint32_t flags, uint32_t seen) {
+  const u32x4 x = {ones<BF16>(flags, 0), ones<BF16>(flags, 2), ones<BF16>(flags, 4), ones<BF16>(flags, 6)};
+  const u32x4 y = {ones<BF16>(seen, 0), ones<BF16>(seen, 2), ones<BF16>(seen, 4), ones<BF16>(seen, 6)};
+  const f32x4 n = mfma<BF16>(x, y, f32x4{0, 0, 0, 0});
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (n[r] > 0) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[c][r] = __uint_as_float(0x7fc00000u);
+    }
+}
+
+// V's operand of a pair of chunks (dims 8i + 2B and 8i + 2B + 1 for lane i of 16) from four tokens' words: tokens 0 and 1 to one
+// register, 2 and 3 to the next.
+template <bool BF16, int B>
+__device__ __forceinline__ void unpack_v(u32x4 v, const float (&power)[4], uint32_t (&even)[2], uint32_t (&odd)[2]) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const uint32_t x = unpack2<BF16, B>(v[2 * p], power[2 * p]), y = unpack2<BF16, B>(v[2 * p + 1], power[2 * p + 1]);
+    even[p] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+    odd[p] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+  }
+}
+__device__ __forceinline__ void powers(uint32_t ve, float (&p)[4]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) p[r] = power_of(ve >> (8 * r) & 255);
+}
+
+// ---- Softmax of a row's scores.
+
+template <int N>
+__device__ __forceinline__ void rescale(f32x4 (&o)[8], float& ref, float& sum, float top, float c) {
+  // a wave-wide decision: nearly always no row's score passes its reference by kRoom
+  if (__any(top * c > ref + kRoom)) {
+    const float to = fmaxf(ref, row_max(top) * c - kBelow), f = __builtin_amdgcn_exp2f(ref - to);
+    sum *= f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] *= f;
+    ref = to;
+  }
+}
+
+// ---- What a row leaves.
+
+__device__ __forceinline__ void row_place(const AttendArgs& a, const Walk& w, int n, int64_t& at) {
+  const int token = w.q.first + n / a.s.g, head = w.h * a.s.g + n % a.s.g;
+  at = (w.l * a.s.n_q + token) * (int64_t)(a.s.H * a.s.g) + head;
+}
+__device__ __forceinline__ float row_lse(float ref, float sum) {
+  return sum == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+__device__ __forceinline__ float row_scale(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+
+// The 16 bytes of a row of q that lane (row, quarter) holds for the step s of K's dims.
+__device__ __forceinline__ u32x4 load_q(const AttendArgs& a, const Walk& w, int n, int quarter, int s) {
+  if (n >= w.q.rows) return u32x4{0, 0, 0, 0};
+  const int token = w.q.first + n / a.s.g, head = w.h * a.s.g + n % a.s.g;
+  return *(const u32x4*)(a.q + w.l * a.q_layer_stride_b + token * a.q_token_stride_b + (head * 128 + quarter * 32 + s * 8) * 2);
+}
+
+// ---- Few rows: every wave has all of an item's rows and every fourth run of 32 tokens.
+
+template <int RT>
+struct RowsLds {
+  FindLds find;
+  float ref[kWaves][16 * RT], sum[kWaves][16 * RT];
+  float o[kWaves][16][132];
+};
+
+template <bool BF16, int RT>
+__global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(AttendArgs a) {
+  __shared__ RowsLds<RT> lds;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+  // neighbouring stretches to one XCD: row tiles of a request and head read the same cache
+  const int64_t wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  Walk w;
+  if (!find(a, lds.find, wg, w)) return;
+  const int per = a.s.unit / kPairTokens;
+  for (;;) {
+    const int64_t left = w.end - w.at;
+    const int u1 = w.item.units - w.u < left ? w.item.units : w.u + (int)left;
+    const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
+    const char* layer = a.cache + w.l * a.cache_layer_stride;
+    const int32_t* table = a.tables + (w.l * a.s.R + w.r) * a.s.E;
+
+    u32x4 q[RT][4];
+    f32x4 o[RT][8];
+    float ref[RT], sum[RT];
+    int low[RT], high[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int n = w.t * 16 * RT + 16 * t + col;
+      const int pos = w.q.ctx - w.q.len + n / a.s.g;
+      low[t] = attend_low(a.s, pos), high[t] = n < w.q.rows ? attend_high(a.s, pos) : 0;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) q[t][s] = load_q(a, w, n, quarter, s);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
+      ref[t] = kNothing, sum[t] = 0.f;
+    }
+
+    const auto load = [&](Tile (&x)[2], bool (&there)[2], int pair) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_tile(x[j], record(a, table, layer, w.h, 2 * pair + j, there[j]), lane);
+    };
+    const auto attend = [&](const Tile (&x)[2], const bool (&there)[2], int pair) {
+      f32x4 s[RT][2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float power = power_of(x[j].ke);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const u32x4 k = unpack8<BF16>(x[j].k[d], power);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) s[t][j] = mfma<BF16>(k, q[t][d], s[t][j]);
+        }
+      }
+      const int pos = pair * kPairTokens;
+      uint32_t ve[2] = {x[0].ve, x[1].ve};
+      // every row sees all 32 tokens, but at the ends of what the rows see and where the table has a hole
+      if (pos < w.item.low_max || pos + kPairTokens > w.item.high_min || !there[0] || !there[1]) {
+        uint32_t flags = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          ve[j] = seen_only(ve[j], pos + 16 * j + 4 * quarter, there[j], w.item);
+          const uint32_t f = nan_bytes(ve[j]);
+          ve[j] = without_nans(ve[j], f);
+          flags |= f << (4 * j);
+        }
+        const bool any = __any(flags != 0);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          uint32_t seen = 0;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int p = pos + 16 * j + 4 * quarter + r;
+              if (there[j] && p >= low[t] && p < high[t])
+                seen |= 1u << (4 * j + r);
+              else
+                s[t][j][r] = -__builtin_inff();
+            }
+          if (any) poison<BF16>(o[t], flags, seen);
+        }
+      }
+      u32x4 hi[RT], lo[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float top = s[t][0][0];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
+        rescale<8>(o[t], ref[t], sum[t], top, a.c);
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], a.c, -ref[t]));
+        sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        // a probability as the sum of two 16-bit numbers: the matrix cores have the time for the second product here, and the
+        // only rounding that counts is then that of the output
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          hi[t][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
+          lo[t][j] = pack2<BF16>(p[2 * j] - low16<BF16>(hi[t][j]), p[2 * j + 1] - high16<BF16>(hi[t][j]));
+        }
+      }
+      float p0[4], p1[4];
+      powers(ve[0], p0);
+      powers(ve[1], p1);
+      const auto chunks = [&](auto b) {
+        constexpr int B = decltype(b)::value;
+        uint32_t e0[2], d0[2], e1[2], d1[2];
+        unpack_v<BF16, B>(x[0].v, p0, e0, d0);
+        unpack_v<BF16, B>(x[1].v, p1, e1, d1);
+        const u32x4 even = {e0[0], e0[1], e1[0], e1[1]}, odd = {d0[0], d0[1], d1[0], d1[1]};
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          o[t][2 * B] = mfma<BF16>(even, hi[t], o[t][2 * B]);
+          o[t][2 * B + 1] = mfma<BF16>(odd, hi[t], o[t][2 * B + 1]);
+          o[t][2 * B] = mfma<BF16>(even, lo[t], o[t][2 * B]);
+          o[t][2 * B + 1] = mfma<BF16>(odd, lo[t], o[t][2 * B + 1]);
+        }
+      };
+      chunks(std::integral_constant<int, 0>{});
+      chunks(std::integral_constant<int, 1>{});
+      chunks(std::integral_constant<int, 2>{});
+      chunks(std::integral_constant<int, 3>{});
+    };
+
+    Tile x[2], y[2];
+    bool tx[2], ty[2];
+    int pair = pa + wave;
+    if (pair < pb) load(x, tx, pair);
+    while (pair < pb) {
+      if (pair + kWaves < pb) load(y, ty, pair + kWaves);
+      attend(x, tx, pair);
+      pair += kWaves;
+      if (pair >= pb) break;
+      if (pair + kWaves < pb) load(x, tx, pair + kWaves);
+      attend(y, ty, pair);
+      pair += kWaves;
+    }
+
+    // the four waves' sums, under the largest of their references
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      sum[t] = row_sum(sum[t]);
+      if (quarter == 0) lds.ref[wave][16 * t + col] = ref[t], lds.sum[wave][16 * t + col] = sum[t];
+    }
+    __syncthreads();
+    const bool whole = w.u == 0 && u1 == w.item.units;
+    float* part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(16 * RT));
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      float top = kNothing;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) top = fmaxf(top, lds.ref[v][16 * t + col]);
+      const float f = __builtin_amdgcn_exp2f(ref[t] - top);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float* to = &lds.o[wave][col][(4 * quarter + r) * 8];
+        *(f32x4*)to = f32x4{o[t][0][r], o[t][1][r], o[t][2][r], o[t][3][r]} * f;
+        *(f32x4*)(to + 4) = f32x4{o[t][4][r], o[t][5][r], o[t][6][r], o[t][7][r]} * f;
+      }
+      __syncthreads();
+      // a thread adds eight dims of a row
+      const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8, n = w.t * 16 * RT + 16 * t + row;
+      float m = kNothing, all = 0.f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) m = fmaxf(m, lds.ref[v][16 * t + row]);
+      f32x4 y0 = {0, 0, 0, 0}, y1 = {0, 0, 0, 0};
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        all += lds.sum[v][16 * t + row] * __builtin_amdgcn_exp2f(lds.ref[v][16 * t + row] - m);
+        y0 += *(const f32x4*)&lds.o[v][row][d];
+        y1 += *(const f32x4*)&lds.o[v][row][d + 4];
+      }
+      if (n < w.q.rows) {
+        if (whole) {
+          const float f1 = row_scale(all);
+          int64_t at;
+          row_place(a, w, n, at);
+          y0 *= f1, y1 *= f1;
+          *(u32x4*)(a.out + (at * 128 + d) * 2) = u32x4{pack2<BF16>(y0[0], y0[1]), pack2<BF16>(y0[2], y0[3]), pack2<BF16>(y1[0], y1[1]), pack2<BF16>(y1[2], y1[3])};
+          if (d == 0 && a.lse) a.lse[at] = row_lse(m, all);
+        } else {
+          *(f32x4*)(part + (16 * t + row) * 128 + d) = y0;
+          *(f32x4*)(part + (16 * t + row) * 128 + d + 4) = y1;
+          if (d == 0) {
+            part[16 * RT * 128 + (16 * t + row) * 2] = m;
+            part[16 * RT * 128 + (16 * t + row) * 2 + 1] = all;
+          }
+        }
+      }
+      __syncthreads();
+    }
+    w.at += u1 - w.u;
+    if (w.at >= w.end) return;
+    next_item(a, w);
+  }
+}
+
+// ---- Many rows: every wave has 32 of an item's 128 rows, and the workgroup turns 64 tokens at a time into operands in LDS.
+
+struct ManyLds {
+  FindLds find;
+  u32x4 k[2][4][4][64];  // [buffer][16 tokens][step of the dims][lane]
+  u32x2 v[2][2][8][64][2];  // [buffer][32 tokens][chunk][lane][16 tokens of the 32]
+  uint32_t ve[2][4][16];    // V's exponent words of the tiles of a buffer at the ends of what the rows see
+  int32_t there[2][4];
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) {
+  constexpr int RT = 2, kStep = 64, kRows = 128;
+  __shared__ ManyLds lds;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+  const int64_t wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  Walk w;
+  if (!find(a, lds.find, wg, w)) return;
+  const int per = a.s.unit / kPairTokens;
+  for (;;) {
+    const int64_t left = w.end - w.at;
+    const int u1 = w.item.units - w.u < left ? w.item.units : w.u + (int)left;
+    const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
+    const char* layer = a.cache + w.l * a.cache_layer_stride;
+    const int32_t* table = a.tables + (w.l * a.s.R + w.r) * a.s.E;
+    const int steps = (pb - pa + 1) / 2, row0 = w.t * kRows + wave * 16 * RT;
+    const bool busy = row0 < w.q.rows;
+
+    u32x4 q[RT][4];
+    f32x4 o[RT][8];
+    float ref[RT], sum[RT];
+    int low[RT], high[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int n = row0 + 16 * t + col;
+      const int pos = w.q.ctx - w.q.len + n / a.s.g;
+      low[t] = attend_low(a.s, pos), high[t] = n < w.q.rows ? attend_high(a.s, pos) : 0;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) q[t][s] = load_q(a, w, n, quarter, s);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
+      ref[t] = kNothing, sum[t] = 0.f;
+    }
+
+    const auto at_ends = [&](int pos) { return pos < w.item.low_max || pos + kStep > w.item.high_min; };
+    // the wave's 16 tokens of a step
+    const auto load = [&](Tile& x, bool& there, int step) {
+      const int pair = pa + 2 * step + (wave >> 1);
+      bool in = pair < pb;
+      const char* rec = record(a, table, layer, w.h, in ? 2 * pair + (wave & 1) : 2 * pa, there);
+      there = there && in;
+      load_tile(x, rec, lane);
+    };
+    const auto unpack = [&](const Tile& x, bool there, int step, int buf) {
+      const int pos = (pa + 2 * step) * kPairTokens;
+      uint32_t ve = x.ve;
+      if (at_ends(pos) || !there) {
+        ve = seen_only(ve, pos + 16 * wave + 4 * quarter, there, w.item);
+        if ((col & 3) == 0) lds.ve[buf][wave][quarter * 4 + (col >> 2)] = ve;
+        ve = without_nans(ve, nan_bytes(ve));
+      }
+      if (lane == 0) lds.there[buf][wave] = there;
+      const float power = power_of(x.ke);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) lds.k[buf][wave][d][lane] = unpack8<BF16>(x.k[d], power);
+      float p[4];
+      powers(ve, p);
+      const auto chunks = [&](auto b) {
+        constexpr int B = decltype(b)::value;
+        uint32_t e[2], d[2];
+        unpack_v<BF16, B>(x.v, p, e, d);
+        lds.v[buf][wave >> 1][2 * B][lane][wave & 1] = u32x2{e[0], e[1]};
+        lds.v[buf][wave >> 1][2 * B + 1][lane][wave & 1] = u32x2{d[0], d[1]};
+      };
+      chunks(std::integral_constant<int, 0>{});
+      chunks(std::integral_constant<int, 1>{});
+      chunks(std::integral_constant<int, 2>{});
+      chunks(std::integral_constant<int, 3>{});
+    };
+    const auto attend = [&](int step, int buf) {
+      const int pos = (pa + 2 * step) * kPairTokens;
+      f32x4 s[RT][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const u32x4 k = lds.k[buf][j][d][lane];
+#pragma unroll
+          for (int t = 0; t < RT; ++t) s[t][j] = mfma<BF16>(k, q[t][d], s[t][j]);
+        }
+      }
+      const int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
+      const bool ends = at_ends(pos);
+      if (ends || there != 15) {
+        uint32_t flags = 0;
+        if (ends) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) flags |= nan_bytes(lds.ve[buf][j][quarter * 4 + (col >> 2)]) << (4 * j);
+        }
+        const bool any = __any(flags != 0);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          uint32_t seen = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int p = pos + 16 * j + 4 * quarter + r;
+              if ((there >> j & 1) && p >= low[t] && p < high[t])
+                seen |= 1u << (4 * j + r);
+              else
+                s[t][j][r] = -__builtin_inff();
+            }
+          if (any) {
+            poison<BF16>(o[t], flags & 255, seen & 255);
+            poison<BF16>(o[t], flags >> 8, seen >> 8);
+          }
+        }
+      }
+      u32x4 p16[RT][2];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float top = s[t][0][0];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
+        rescale<8>(o[t], ref[t], sum[t], top, a.c);
+        float p[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], a.c, -ref[t]));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sum[t] += p[2 * j] + p[2 * j + 1];
+          p16[t][j >> 2][j & 3] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const u32x4 v = *(const u32x4*)&lds.v[buf][j][c][lane][0];
+#pragma unroll
+          for (int t = 0; t < RT; ++t) o[t][c] = mfma<BF16>(v, p16[t][j], o[t][c]);
+        }
+    };
+
+    Tile x;
+    bool there;
+    if (steps > 0) {
+      load(x, there, 0);
+      unpack(x, there, 0, 0);
+    }
+    __syncthreads();
+    for (int step = 0; step < steps; ++step) {
+      const bool more = step + 1 < steps;
+      if (more) load(x, there, step + 1);
+      if (busy) attend(step, step & 1);
+      if (more) unpack(x, there, step + 1, (step + 1) & 1);
+      __syncthreads();
+    }
+
+    const bool whole = w.u == 0 && u1 == w.item.units;
+    float* part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(kRows));
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float all = row_sum(sum[t]);
+      const int m = wave * 16 * RT + 16 * t + col, n = w.t * kRows + m;
+      if (n >= w.q.rows) continue;
+      if (whole) {
+        const float f = row_scale(all);
+        int64_t at;
+        row_place(a, w, n, at);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *(u32x4*)(a.out + (at * 128 + (4 * quarter + r) * 8) * 2) =
+              u32x4{pack2<BF16>(o[t][0][r] * f, o[t][1][r] * f), pack2<BF16>(o[t][2][r] * f, o[t][3][r] * f),
+                    pack2<BF16>(o[t][4][r] * f, o[t][5][r] * f), pack2<BF16>(o[t][6][r] * f, o[t][7][r] * f)};
+        if (quarter == 0 && a.lse) a.lse[at] = row_lse(ref[t], all);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          *(f32x4*)(part + m * 128 + (4 * quarter + r) * 8) = f32x4{o[t][0][r], o[t][1][r], o[t][2][r], o[t][3][r]};
+          *(f32x4*)(part + m * 128 + (4 * quarter + r) * 8 + 4) = f32x4{o[t][4][r], o[t][5][r], o[t][6][r], o[t][7][r]};
+        }
+        if (quarter == 0) part[kRows * 128 + m * 2] = ref[t], part[kRows * 128 + m * 2 + 1] = all;
+      }
+    }
+    w.at += u1 - w.u;
+    if (w.at >= w.end) return;
+    next_item(a, w);
+  }
+}
+
+// ---- Items that were cut: a workgroup per border between two stretches and row joins the parts of the item that the border cuts, if
+// it is the item's first such border.
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+  __shared__ float o[kWaves][128], tops[kWaves], sums[kWaves];
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+  const int64_t total = a.before[a.s.R], line = total * a.s.L, share = attend_share(a.s, line);
+  const int64_t border = ((int64_t)blockIdx.x + 1) * share;
+  if (border >= line) return;
+  Walk w;
+  w.l = border / total;
+  int64_t rest = border - w.l * total;
+  int64_t lo = 0, hi = a.s.R;  // the last request that begins at or before: requests without units begin where the next one does
+  while (hi - lo > 1) {
+    const int64_t mid = (lo + hi) / 2;
+    if (a.before[mid] <= rest)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  w.r = (int)lo;
+  rest -= a.before[lo];
+  w.q = request(a, w.r);
+  const int64_t units = attend_units(a.s, w.q);
+  w.h = (int)(rest / units);
+  rest -= w.h * units;
+  for (w.t = 0;; ++w.t) {
+    w.item = attend_item(a.s, w.q, w.t);
+    if (rest < w.item.units) break;
+    rest -= w.item.units;
+  }
+  const int64_t begin = border - rest, end = begin + w.item.units;
+  const int m = blockIdx.y, n = w.t * a.s.rows + m;
+  if (rest == 0 || border - share > begin || n >= w.q.rows) return;
+  const int64_t first = border / share - 1, last = (end - 1) / share;
+  const auto part = [&](int64_t g) {
+    return (const float*)(a.parts + attend_place(g, g > first || first * share == begin) * (int64_t)attend_part_bytes(a.s.rows));
+  };
+  const int stats = a.s.rows * 128 + 2 * m;
+  float top = kNothing;
+  for (int64_t g = first + threadIdx.x; g <= last; g += kThreads) top = fmaxf(top, part(g)[stats]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) top = fmaxf(top, tops[v]);
+  float x = 0.f, y = 0.f, sum = 0.f;
+#pragma unroll 4
+  for (int64_t g = first + wave; g <= last; g += kWaves) {
+    const float* p = part(g);
+    const float f = __builtin_amdgcn_exp2f(p[stats] - top);
+    const float2 v = *(const float2*)(p + m * 128 + 2 * lane);
+    sum = fmaf(p[stats + 1], f, sum);
+    x = fmaf(v.x, f, x);
+    y = fmaf(v.y, f, y);
+  }
+  o[wave][2 * lane] = x, o[wave][2 * lane + 1] = y;
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  if (wave) return;
+  sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  const float f = row_scale(sum);
+  x = ((o[0][2 * lane] + o[1][2 * lane]) + (o[2][2 * lane] + o[3][2 * lane])) * f;
+  y = ((o[0][2 * lane + 1] + o[1][2 * lane + 1]) + (o[2][2 * lane + 1] + o[3][2 * lane + 1])) * f;
+  int64_t at;
+  row_place(a, w, n, at);
+  *(uint32_t*)(a.out + (at * 128 + 2 * lane) * 2) = pack2<BF16>(x, y);
+  if (lane == 0 && a.lse) a.lse[at] = row_lse(top, sum);
+}
+
+rc_status attend_check(const rc_cache_desc* d, int64_t R, int64_t E, int32_t n_heads, int64_t n_q, int64_t max_q, int64_t window, AttendShape* s,
+                       const char* who) {
+  if (rc_status e = check_cache(d, who)) return e;
+  if (R < 0 || E < 0 || n_q < 0 || max_q < 0 || window < 0) return fail(RC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (n_heads < 1 || n_heads % d->n_kv_heads != 0)
+    return fail(RC_ERR_INVALID_ARG, "%s: n_heads %d is not a multiple of n_kv_heads %d", who, n_heads, d->n_kv_heads);
+  if (n_heads > 1024) return fail(RC_ERR_UNSUPPORTED, "%s: n_heads %d (at most 1024)", who, n_heads);
+  if (!attend_shape(s, d->n_layers, R, d->n_blocks ? E : 0, d->block_tokens, d->n_kv_heads, n_heads, n_q, max_q, window))
+    return fail(RC_ERR_UNSUPPORTED, "%s: more than 2^31 positions, rows or requests", who);
+  return RC_OK;
+}
+
+template <bool BF16>
+void attend_launch(const AttendArgs& a, hipStream_t st) {
+  const dim3 grid(a.s.wgs);
+  if (a.s.rows == 16)
+    attend_rows_kernel<BF16, 1><<<grid, kThreads, 0, st>>>(a);
+  else if (a.s.rows == 32)
+    attend_rows_kernel<BF16, 2><<<grid, kThreads, 0, st>>>(a);
+  else
+    attend_many_kernel<BF16><<<grid, kThreads, 0, st>>>(a);
+  if (a.before) {
+    const int64_t rows = (int64_t)a.s.max_q * a.s.g;
+    attend_join_kernel<BF16><<<dim3(a.s.wgs - 1, (unsigned)(rows < a.s.rows ? rows : a.s.rows)), kThreads, 0, st>>>(a);
+  }
+}
+
+}  // namespace
+}  // namespace rc
+
+extern "C" size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int64_t R, int64_t E, int32_t n_heads, int64_t max_q) {
+  using namespace rc;
+  clear_error();
+  AttendShape s;
+  if (attend_check(desc, R, E, n_heads, max_q, max_q, 0, &s, "rc_cache_attend_workspace_size")) return 0;
+  if (attend_most_parts(s) == 0) return 0;
+  // the tiles of fewer rows have smaller parts, but not fewer in all: the largest of them up to this max_q
+  return attend_header_bytes(R) + (size_t)attend_most_parts(s) * attend_part_bytes(s.rows);
+}
+
+extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const int32_t* tables, int64_t R, int64_t E,
+                                     const int32_t* ctx_len, const int32_t* q_start, const void* q, int64_t n_q, int32_t n_heads,
+                                     int64_t q_token_stride, int64_t q_layer_stride, int64_t max_q, float scale, int64_t window,
+                                     void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace rc;
+  const char* who = "rc_cache_attend";
+  clear_error();
+  AttendArgs a;
+  if (rc_status e = attend_check(desc, R, E, n_heads, n_q, max_q, window, &a.s, who)) return e;
+  if (!q_start && (max_q > 1 || n_q < R)) return fail(RC_ERR_INVALID_ARG, "%s: without q_start there is one query token per request", who);
+  if (!(scale > 0.f) || scale > 3e38f) return fail(RC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  if (desc->n_layers == 0 || R == 0 || n_q == 0 || max_q == 0) return RC_OK;
+  const bool empty = a.s.cap == 0;  // nothing to see: no table and no cache are read
+  if (!ctx_len || !q || !out || (!empty && (!cache || !tables))) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (!aligned16(q) || !aligned16(out) || (!empty && !aligned16(cache))) return fail(RC_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+  if (q_token_stride < (int64_t)n_heads * 128 || q_token_stride > INT64_MAX / 4 / n_q || q_token_stride % 8 != 0 || q_layer_stride % 8 != 0)
+    return fail(RC_ERR_INVALID_ARG, "%s: q_token_stride smaller than n_heads*Dh, or a stride that breaks 16-byte alignment", who);
+  if (desc->n_layers > 1 && q_layer_stride < (int64_t)n_heads * 128) return fail(RC_ERR_INVALID_ARG, "%s: q_layer_stride smaller than a token", who);
+  const int64_t parts = attend_most_parts(a.s);
+  if (parts) {
+    const size_t need = attend_header_bytes(R) + (size_t)parts * attend_part_bytes(a.s.rows);
+    if (!workspace || workspace_bytes < need) return fail(RC_ERR_WORKSPACE, "%s: needs %zu bytes of workspace", who, need);
+    if (!aligned16(workspace)) return fail(RC_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
+  }
+  a.cache = (const char*)cache, a.tables = tables, a.ctx_len = ctx_len, a.q_start = q_start;
+  a.q = (const char*)q, a.out = (char*)out, a.lse = lse;
+  a.cache_layer_stride = desc->layer_stride, a.q_token_stride_b = q_token_stride * 2, a.q_layer_stride_b = q_layer_stride * 2;
+  a.n_blocks = desc->n_blocks;
+  a.c = scale * 1.4426950408889634f;
+  a.before = parts ? (int64_t*)workspace : nullptr;
+  a.parts = parts ? (char*)workspace + attend_header_bytes(R) : nullptr;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (desc->dtype == RC_BF16)
+    attend_launch<true>(a, st);
+  else
+    attend_launch<false>(a, st);
+  return check_launch(who);
+}

@@ -1,0 +1,135 @@
+// How the work of rc_cache_attend is cut into equal shares.  Plain C++ (host and device), so that the arithmetic can be checked
+// where there is no GPU.
+//
+// The query tokens of a request times the query heads of one KV head are its rows, in tiles of `rows` rows.  An item is one row
+// tile of one request and KV head of one layer; its work is the run of cached tokens that its rows see, in units of
+// `unit` tokens.  All units of a call, item after item (layer, request, head, tile), are one line, and every workgroup
+// takes an equal stretch of it, whatever the lengths of the requests are.  Where a stretch ends inside an item, the parts are
+// joined by a second launch.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#ifdef __HIPCC__
+#define RC_HD __host__ __device__
+#else
+#define RC_HD
+#endif
+
+namespace rc {
+
+constexpr int kPairTokens = 32;  // what a wave takes at a time; items begin at a multiple of it
+
+// The shape of a call, and of its kernel's tiles.
+struct AttendShape {
+  int64_t L, R, E;
+  int32_t T, H, g;     // tokens of a block, KV heads, query heads of a KV head
+  int32_t n_q, max_q;  // query tokens of a layer, of a request at most
+  int32_t window;      // 0: none
+  int32_t rows, unit;  // rows of a tile, tokens of a unit
+  int32_t cap;         // positions of a table, E * T
+  int32_t least;       // units of a stretch, at least
+  int32_t wgs;         // workgroups
+};
+
+// A request's query tokens, row tiles and cached tokens, from what the device arrays hold (anything at all).
+struct AttendRequest {
+  int32_t first, len, rows, tiles, ctx;
+};
+RC_HD inline AttendRequest attend_request(const AttendShape& s, int32_t ctx, int32_t start, int32_t end) {
+  AttendRequest q;
+  q.first = start < 0 ? 0 : start > s.n_q ? s.n_q : start;
+  const int32_t stop = end < q.first ? q.first : end > s.n_q ? s.n_q : end;
+  q.len = stop - q.first;
+  q.ctx = ctx < 0 ? 0 : ctx;
+  // tokens beyond the longest that the host told of keep their places but are not computed
+  q.rows = (q.len < s.max_q ? q.len : s.max_q) * s.g;
+  q.tiles = (q.rows + s.rows - 1) / s.rows;
+  return q;
+}
+
+// The cached tokens of a row tile.  Row n of a request is query token n / g, at position ctx - len + n / g.
+struct AttendItem {
+  int32_t pair0, pairs;      // first run of 32 tokens, number of runs
+  int32_t units;             // at least 1: an item that sees nothing still has to say so
+  int32_t low_min, low_max;  // first position seen by the first and by the last row
+  int32_t high_min, high_max;  // one past the last position seen by the first and by the last row
+};
+RC_HD inline int32_t attend_low(const AttendShape& s, int32_t pos) {
+  return s.window && pos >= s.window ? pos - s.window + 1 : 0;
+}
+RC_HD inline int32_t attend_high(const AttendShape& s, int32_t pos) { return pos < 0 ? 0 : pos < s.cap ? pos + 1 : s.cap; }
+RC_HD inline AttendItem attend_item(const AttendShape& s, const AttendRequest& q, int32_t tile) {
+  const int32_t n0 = tile * s.rows, n1 = (q.rows - n0 < s.rows ? q.rows : n0 + s.rows) - 1;
+  const int32_t p0 = q.ctx - q.len + n0 / s.g, p1 = q.ctx - q.len + n1 / s.g;
+  AttendItem i;
+  i.low_min = attend_low(s, p0), i.low_max = attend_low(s, p1);
+  i.high_min = attend_high(s, p0), i.high_max = attend_high(s, p1);
+  i.pair0 = i.low_min / kPairTokens;
+  const int32_t end = (int32_t)(((int64_t)i.high_max + kPairTokens - 1) / kPairTokens);
+  i.pairs = end > i.pair0 ? end - i.pair0 : 0;
+  const int32_t per = s.unit / kPairTokens;
+  i.units = i.pairs ? (i.pairs + per - 1) / per : 1;
+  return i;
+}
+
+// Units of a request and KV head.
+RC_HD inline int64_t attend_units(const AttendShape& s, const AttendRequest& q) {
+  int64_t n = 0;
+  for (int32_t t = 0; t < q.tiles; ++t) n += attend_item(s, q, t).units;
+  return n;
+}
+
+// Units of a workgroup's stretch where there are `total` of them.
+RC_HD inline int64_t attend_share(const AttendShape& s, int64_t total) {
+  const int64_t n = (total + s.wgs - 1) / s.wgs;
+  return n < s.least ? s.least : n;
+}
+
+// Where a part of an item that is cut is kept: two places per workgroup, one for the part that its stretch begins with, one for a
+// part that begins later (and that the stretch then ends with).
+RC_HD inline int64_t attend_place(int64_t wg, bool begins) { return 2 * wg + (begins ? 0 : 1); }
+
+// The workspace: units before each request (int64 [R + 1]), then the parts, rows x (128 sums, reference, sum of weights) in fp32.
+inline size_t attend_header_bytes(int64_t R) { return ((size_t)(R + 1) * 8 + 255) / 256 * 256; }
+RC_HD inline size_t attend_part_bytes(int32_t rows) { return (size_t)rows * 130 * 4; }
+
+constexpr int kWholeTokens = 1024;
+
+struct AttendKernel {
+  int32_t rows, unit, wgs, least;
+};
+// Kernels by the rows of a request and KV head (query tokens times heads of a KV head): tiles of 16 and 32 rows, where every wave
+// of a workgroup has all rows and a quarter of the tokens, and of 128, where every wave has a quarter of the rows.
+inline AttendKernel attend_kernel(int64_t rows) {
+  if (rows <= 16) return {16, 128, 768, 4};
+  if (rows <= 32) return {32, 128, 512, 4};
+  return {128, 64, 512, 8};
+}
+
+// Most units of an item, whatever the lengths: an item of a table's whole length that begins anywhere.
+inline int64_t attend_most_units(const AttendShape& s) {
+  const int64_t pairs = ((int64_t)s.cap + kPairTokens - 1) / kPairTokens, per = s.unit / kPairTokens;
+  const int64_t n = (pairs + per - 1) / per;
+  return n < 1 ? 1 : n;
+}
+
+// The shape of a call; false where it is beyond what the kernels count in 32 bits.
+inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_t T, int32_t H, int32_t n_heads, int64_t n_q, int64_t max_q,
+                         int64_t window) {
+  const int32_t g = n_heads / H;
+  if (max_q > n_q) max_q = n_q;
+  if (E > (0x7fffffffLL - 64) / T || n_q > 0x7fffffffLL / 2 || R > 0x7fffffffLL / 2 || (max_q > 0 && max_q > 0x7fffff00LL / g)) return false;
+  const AttendKernel k = attend_kernel(max_q * g);
+  // a window longer than any position is none
+  *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.wgs};
+  // a short table: items are not cut, and nothing has to be joined
+  if (s->cap <= kWholeTokens) s->unit = (s->cap + k.unit - 1) / k.unit * k.unit + k.unit, s->least = 1;
+  // no more workgroups than there can be stretches
+  const double items = (double)L * R * H * (((double)max_q * g + k.rows - 1) / k.rows), most = items * attend_most_units(*s) / s->least + 1;
+  if (most < s->wgs) s->wgs = ((int32_t)most + 8) / 8 * 8;
+  return true;
+}
+inline int64_t attend_most_parts(const AttendShape& s) { return attend_most_units(s) > 1 ? 2 * (int64_t)s.wgs : 0; }
+
+}  // namespace rc

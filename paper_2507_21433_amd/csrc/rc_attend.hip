@@ -28,7 +28,7 @@ struct AttendArgs {
   float* lse;
   int64_t cache_layer_stride, q_token_stride_b, q_layer_stride_b, n_blocks;
   float c;  // scale * log2(e)
-  int64_t* before;  // units before each request, [R + 1]; NULL where nothing is joined
+  AttendBorder* borders;  // NULL where no item is cut
   char* parts;
 };
 
@@ -94,7 +94,7 @@ struct FindLds {
 };
 
 struct Walk {
-  int64_t at, end, begin;  // units of the line
+  int64_t at, end, begin, share;  // units of the line
   int64_t l;
   int r, h, t, u;  // layer, request, head, row tile, unit of the item
   AttendRequest q;
@@ -129,14 +129,16 @@ __device__ inline bool find(const AttendArgs& a, FindLds& lds, int64_t wg, Walk&
     const int64_t r = base + threadIdx.x;
     mine = r < a.s.R ? attend_units(a.s, request(a, (int)r)) * a.s.H : 0;
     upto = block_scan(mine, lds, all) + total;
-    if (wg == 0 && a.before && r < a.s.R) a.before[r] = upto - mine;
     total += all;
   }
-  if (wg == 0 && a.before && threadIdx.x == 0) a.before[a.s.R] = total;
   const int64_t line = total * a.s.L, share = attend_share(a.s, line);
   w.begin = w.at = wg * share;
   w.end = w.at + share < line ? w.at + share : line;
-  if (w.at >= w.end) return false;
+  w.share = share;
+  if (w.at >= w.end) {
+    if (a.borders && threadIdx.x == 0) a.borders[wg].last = -1;
+    return false;
+  }
   w.l = w.at / total;
   const int64_t off = w.at - w.l * total;
   if (a.s.R > kThreads) total = 0;
@@ -182,6 +184,15 @@ __device__ inline void next_item(const AttendArgs& a, Walk& w) {
     }
   }
   w.item = attend_item(a.s, w.q, w.t);
+}
+
+// At the end of a stretch, whose last part ends at unit u1 of its item.
+__device__ inline void leave_border(const AttendArgs& a, int64_t wg, const Walk& w, int u1) {
+  if (!a.borders || threadIdx.x != 0) return;
+  AttendBorder b = {-1, 0, 0, 0, 0, 0, {0, 0}};
+  if (w.u == 0 && u1 < w.item.units)
+    b = {(int32_t)(wg + (w.item.units - u1 + w.share - 1) / w.share), w.at == w.begin, (int32_t)w.l, w.r, w.h, w.t, {0, 0}};
+  a.borders[wg] = b;
 }
 
 // ---- Loads.
@@ -499,8 +510,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       }
       __syncthreads();
     }
+    if (w.at + (u1 - w.u) >= w.end) {
+      leave_border(a, wg, w, u1);
+      return;
+    }
     w.at += u1 - w.u;
-    if (w.at >= w.end) return;
     next_item(a, w);
   }
 }
@@ -693,82 +707,84 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         if (quarter == 0) part[kRows * 128 + m * 2] = ref[t], part[kRows * 128 + m * 2 + 1] = all;
       }
     }
+    if (w.at + (u1 - w.u) >= w.end) {
+      leave_border(a, wg, w, u1);
+      return;
+    }
     w.at += u1 - w.u;
-    if (w.at >= w.end) return;
     next_item(a, w);
   }
 }
 
-// ---- Items that were cut: a workgroup per border between two stretches and row joins the parts of the item that the border cuts, if
-// it is the item's first such border.
+// ---- Items that were cut: a workgroup joins the parts of the item that begins in a stretch and goes on behind it, some rows at a time.
 
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
-  __shared__ float o[kWaves][128], tops[kWaves], sums[kWaves];
-  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-  const int64_t total = a.before[a.s.R], line = total * a.s.L, share = attend_share(a.s, line);
-  const int64_t border = ((int64_t)blockIdx.x + 1) * share;
-  if (border >= line) return;
-  Walk w;
-  w.l = border / total;
-  int64_t rest = border - w.l * total;
-  int64_t lo = 0, hi = a.s.R;  // the last request that begins at or before: requests without units begin where the next one does
-  while (hi - lo > 1) {
-    const int64_t mid = (lo + hi) / 2;
-    if (a.before[mid] <= rest)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  w.r = (int)lo;
-  rest -= a.before[lo];
-  w.q = request(a, w.r);
-  const int64_t units = attend_units(a.s, w.q);
-  w.h = (int)(rest / units);
-  rest -= w.h * units;
-  for (w.t = 0;; ++w.t) {
-    w.item = attend_item(a.s, w.q, w.t);
-    if (rest < w.item.units) break;
-    rest -= w.item.units;
-  }
-  const int64_t begin = border - rest, end = begin + w.item.units;
-  const int m = blockIdx.y, n = w.t * a.s.rows + m;
-  if (rest == 0 || border - share > begin || n >= w.q.rows) return;
-  const int64_t first = border / share - 1, last = (end - 1) / share;
-  const auto part = [&](int64_t g) {
-    return (const float*)(a.parts + attend_place(g, g > first || first * share == begin) * (int64_t)attend_part_bytes(a.s.rows));
-  };
-  const int stats = a.s.rows * 128 + 2 * m;
-  float top = kNothing;
-  for (int64_t g = first + threadIdx.x; g <= last; g += kThreads) top = fmaxf(top, part(g)[stats]);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if (lane == 0) tops[wave] = top;
-  __syncthreads();
-#pragma unroll
-  for (int v = 0; v < kWaves; ++v) top = fmaxf(top, tops[v]);
-  float x = 0.f, y = 0.f, sum = 0.f;
-#pragma unroll 4
-  for (int64_t g = first + wave; g <= last; g += kWaves) {
-    const float* p = part(g);
-    const float f = __builtin_amdgcn_exp2f(p[stats] - top);
-    const float2 v = *(const float2*)(p + m * 128 + 2 * lane);
-    sum = fmaf(p[stats + 1], f, sum);
+// The sums of row m over the parts first .. last, from the first-th on in steps: x, y for the lane's two dims, and the weights'.
+__device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendBorder& b, int wg, int m, int first, int step, float top, float& x, float& y,
+                                           float& sum) {
+  const int lane = threadIdx.x & 63;
+  x = y = sum = 0.f;
+#pragma unroll 8
+  for (int g = wg + first; g <= b.last; g += step) {
+    const float* p = (const float*)(a.parts + attend_place(g, g > wg || b.begins) * (int64_t)attend_part_bytes(a.s.rows));
+    const float2 s = *(const float2*)(p + a.s.rows * 128 + 2 * m), v = *(const float2*)(p + m * 128 + 2 * lane);
+    const float f = __builtin_amdgcn_exp2f(s.x - top);
+    sum = fmaf(s.y, f, sum);
     x = fmaf(v.x, f, x);
     y = fmaf(v.y, f, y);
   }
-  o[wave][2 * lane] = x, o[wave][2 * lane + 1] = y;
-  if (lane == 0) sums[wave] = sum;
-  __syncthreads();
-  if (wave) return;
-  sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+__device__ __forceinline__ float join_top(const AttendArgs& a, const AttendBorder& b, int wg, int m) {
+  float top = kNothing;
+  for (int g = wg + (threadIdx.x & 63); g <= b.last; g += 64) {
+    const float* p = (const float*)(a.parts + attend_place(g, g > wg || b.begins) * (int64_t)attend_part_bytes(a.s.rows));
+    top = fmaxf(top, p[a.s.rows * 128 + 2 * m]);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  return top;
+}
+template <bool BF16>
+__device__ __forceinline__ void join_store(const AttendArgs& a, const Walk& w, int n, float top, float x, float y, float sum) {
+  const int lane = threadIdx.x & 63;
   const float f = row_scale(sum);
-  x = ((o[0][2 * lane] + o[1][2 * lane]) + (o[2][2 * lane] + o[3][2 * lane])) * f;
-  y = ((o[0][2 * lane + 1] + o[1][2 * lane + 1]) + (o[2][2 * lane + 1] + o[3][2 * lane + 1])) * f;
   int64_t at;
   row_place(a, w, n, at);
-  *(uint32_t*)(a.out + (at * 128 + 2 * lane) * 2) = pack2<BF16>(x, y);
+  *(uint32_t*)(a.out + (at * 128 + 2 * lane) * 2) = pack2<BF16>(x * f, y * f);
   if (lane == 0 && a.lse) a.lse[at] = row_lse(top, sum);
+}
+
+// FEW rows: a workgroup per row, whose waves share the parts (an item of a long context has up to a hundred); else a wave per row.
+template <bool BF16, bool FEW>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+  __shared__ float2 o[kWaves][64];
+  __shared__ float sums[kWaves];
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wg = blockIdx.x;
+  const AttendBorder b = a.borders[wg];
+  if (b.last < 0) return;
+  Walk w;
+  w.l = b.l, w.r = b.r, w.h = b.h, w.t = b.t;
+  w.q = request(a, b.r);
+  const int rows = min(a.s.rows, w.q.rows - b.t * a.s.rows);
+  float x, y, sum;
+  if constexpr (FEW) {
+    const int m = blockIdx.y;
+    if (m >= rows) return;
+    const float top = join_top(a, b, wg, m);
+    join_parts(a, b, wg, m, wave, kWaves, top, x, y, sum);
+    o[wave][lane] = float2{x, y};
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int v = 1; v < kWaves; ++v) x += o[v][lane].x, y += o[v][lane].y, sum += sums[v];
+    join_store<BF16>(a, w, b.t * a.s.rows + m, top, x, y, sum);
+  } else {
+    for (int m = blockIdx.y * kWaves + wave; m < rows; m += gridDim.y * kWaves) {
+      const float top = join_top(a, b, wg, m);
+      join_parts(a, b, wg, m, 0, 1, top, x, y, sum);
+      join_store<BF16>(a, w, b.t * a.s.rows + m, top, x, y, sum);
+    }
+  }
 }
 
 rc_status attend_check(const rc_cache_desc* d, int64_t R, int64_t E, int32_t n_heads, int64_t n_q, int64_t max_q, int64_t window, AttendShape* s,
@@ -792,10 +808,12 @@ void attend_launch(const AttendArgs& a, hipStream_t st) {
     attend_rows_kernel<BF16, 2><<<grid, kThreads, 0, st>>>(a);
   else
     attend_many_kernel<BF16><<<grid, kThreads, 0, st>>>(a);
-  if (a.before) {
-    const int64_t rows = (int64_t)a.s.max_q * a.s.g;
-    attend_join_kernel<BF16><<<dim3(a.s.wgs - 1, (unsigned)(rows < a.s.rows ? rows : a.s.rows)), kThreads, 0, st>>>(a);
-  }
+  if (!a.borders) return;
+  const int64_t rows = (int64_t)a.s.max_q * a.s.g;
+  if (a.s.rows <= 32)
+    attend_join_kernel<BF16, true><<<dim3(a.s.wgs - 1, (unsigned)(rows < a.s.rows ? rows : a.s.rows)), kThreads, 0, st>>>(a);
+  else
+    attend_join_kernel<BF16, false><<<dim3(a.s.wgs - 1, 8), kThreads, 0, st>>>(a);
 }
 
 }  // namespace
@@ -806,9 +824,7 @@ extern "C" size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int6
   clear_error();
   AttendShape s;
   if (attend_check(desc, R, E, n_heads, max_q, max_q, 0, &s, "rc_cache_attend_workspace_size")) return 0;
-  if (attend_most_parts(s) == 0) return 0;
-  // the tiles of fewer rows have smaller parts, but not fewer in all: the largest of them up to this max_q
-  return attend_header_bytes(R) + (size_t)attend_most_parts(s) * attend_part_bytes(s.rows);
+  return attend_workspace(s);
 }
 
 extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const int32_t* tables, int64_t R, int64_t E,
@@ -829,9 +845,8 @@ extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cach
   if (q_token_stride < (int64_t)n_heads * 128 || q_token_stride > INT64_MAX / 4 / n_q || q_token_stride % 8 != 0 || q_layer_stride % 8 != 0)
     return fail(RC_ERR_INVALID_ARG, "%s: q_token_stride smaller than n_heads*Dh, or a stride that breaks 16-byte alignment", who);
   if (desc->n_layers > 1 && q_layer_stride < (int64_t)n_heads * 128) return fail(RC_ERR_INVALID_ARG, "%s: q_layer_stride smaller than a token", who);
-  const int64_t parts = attend_most_parts(a.s);
-  if (parts) {
-    const size_t need = attend_header_bytes(R) + (size_t)parts * attend_part_bytes(a.s.rows);
+  const size_t need = attend_workspace(a.s);
+  if (need) {
     if (!workspace || workspace_bytes < need) return fail(RC_ERR_WORKSPACE, "%s: needs %zu bytes of workspace", who, need);
     if (!aligned16(workspace)) return fail(RC_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
   }
@@ -840,8 +855,8 @@ extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cach
   a.cache_layer_stride = desc->layer_stride, a.q_token_stride_b = q_token_stride * 2, a.q_layer_stride_b = q_layer_stride * 2;
   a.n_blocks = desc->n_blocks;
   a.c = scale * 1.4426950408889634f;
-  a.before = parts ? (int64_t*)workspace : nullptr;
-  a.parts = parts ? (char*)workspace + attend_header_bytes(R) : nullptr;
+  a.borders = need ? (AttendBorder*)workspace : nullptr;
+  a.parts = need ? (char*)workspace + attend_header_bytes(a.s.wgs) : nullptr;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (desc->dtype == RC_BF16)
     attend_launch<true>(a, st);

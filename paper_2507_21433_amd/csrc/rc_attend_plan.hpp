@@ -90,8 +90,14 @@ RC_HD inline int64_t attend_share(const AttendShape& s, int64_t total) {
 // part that begins later (and that the stretch then ends with).
 RC_HD inline int64_t attend_place(int64_t wg, bool begins) { return 2 * wg + (begins ? 0 : 1); }
 
-// The workspace: units before each request (int64 [R + 1]), then the parts, rows x (128 sums, reference, sum of weights) in fp32.
-inline size_t attend_header_bytes(int64_t R) { return ((size_t)(R + 1) * 8 + 255) / 256 * 256; }
+// What a workgroup says of the item that its stretch ends in: where it lies, and up to which workgroup its parts go, if the item begins
+// in this stretch and goes on behind it (else last is -1).
+struct AttendBorder {
+  int32_t last, begins, l, r, h, t, unused[2];
+};
+
+// The workspace: a border per workgroup, then the parts, rows x (128 sums, reference, sum of weights) in fp32.
+RC_HD inline size_t attend_header_bytes(int32_t wgs) { return (size_t)wgs * sizeof(AttendBorder); }
 RC_HD inline size_t attend_part_bytes(int32_t rows) { return (size_t)rows * 130 * 4; }
 
 constexpr int kWholeTokens = 1024;
@@ -130,6 +136,11 @@ inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_
   if (most < s->wgs) s->wgs = ((int32_t)most + 8) / 8 * 8;
   return true;
 }
+// Parts of a call, at most, and its workspace.
 inline int64_t attend_most_parts(const AttendShape& s) { return attend_most_units(s) > 1 ? 2 * (int64_t)s.wgs : 0; }
+inline size_t attend_workspace(const AttendShape& s) {
+  const int64_t parts = attend_most_parts(s);
+  return parts ? attend_header_bytes(s.wgs) + (size_t)parts * attend_part_bytes(s.rows) : 0;
+}
 
 }  // namespace rc

@@ -48,6 +48,14 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   else
     return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
 }
+// Two fp32 numbers to 16-bit ones where the rest is kept as well, so that the direction does not matter.
+template <bool BF16>
+__device__ __forceinline__ uint32_t cut2(float a, float b) {
+  if constexpr (BF16)
+    return pack2<true>(a, b);
+  else
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+}
 template <bool BF16>
 __device__ __forceinline__ float low16(uint32_t w) {
   if constexpr (BF16)
@@ -210,13 +218,19 @@ __device__ __forceinline__ void load_tile(Tile& x, const char* rec, int lane) {
   x.ve = *(const uint32_t*)(rec + kRecordVExp + ((lane >> 4) * 4 + ((lane & 15) >> 2)) * 4);
 }
 
-// The record of the 16 tokens at position 16 * tile (wave-uniform); block 0's where there is no such block (`there` false): its
-// values are replaced or masked.
-__device__ __forceinline__ const char* record(const AttendArgs& a, const int32_t* table, const char* layer, int h, int tile, bool& there) {
-  const int tiles = a.s.T >> 4, e = a.s.T == 32 ? tile >> 1 : tile;
-  const int id = e < a.s.E ? table[e] : -1;
-  there = id >= 0 && id < a.n_blocks;
-  return layer + (((int64_t)(there ? id : 0) * a.s.H + h) * tiles + (a.s.T == 32 ? tile & 1 : 0)) * kRecordBytes;
+// Block ids of the 64 tiles of 16 tokens that a wave will come to next: lane j holds that of the j-th, or -1 where there is no such
+// block.  One load for 64 tiles; taken tile by tile, it would stand in front of the loads of the cache every time.
+__device__ __forceinline__ int load_id(const AttendArgs& a, const int32_t* table, int tile, bool in) {
+  const int e = a.s.T == 32 ? tile >> 1 : tile;
+  const int id = in && e < a.s.E ? table[e] : -1;
+  return id < a.n_blocks ? id : -1;
+}
+// The record of the tile whose id lane j holds (its parity chooses between the records of a block of 32); block 0's where there is no
+// such block (`there` false): its values are replaced or masked.
+__device__ __forceinline__ const char* record(const AttendArgs& a, const char* head, int ids, int j, int parity, bool& there) {
+  const int id = __builtin_amdgcn_readlane(ids, j), tiles = a.s.T >> 4;
+  there = id >= 0;
+  return head + (uint64_t)(uint32_t)(there ? id : 0) * (uint32_t)(a.s.H * tiles * kRecordBytes) + (tiles == 2 ? parity * kRecordBytes : 0);
 }
 
 // V's exponent bytes with those of tokens that no row sees replaced by that of 1: whatever lies there (memory that was never
@@ -278,7 +292,7 @@ __device__ __forceinline__ void unpack_v(u32x4 v, const float (&power)[4], uint3
 }
 __device__ __forceinline__ void powers(uint32_t ve, float (&p)[4]) {
 #pragma unroll
-  for (int r = 0; r < 4; ++r) p[r] = power_of(ve >> (8 * r) & 255);
+  for (int r = 0; r < 4; ++r) p[r] = power_at(ve, r);
 }
 
 // ---- Softmax of a row's scores.
@@ -335,7 +349,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
     const int64_t left = w.end - w.at;
     const int u1 = w.item.units - w.u < left ? w.item.units : w.u + (int)left;
     const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
-    const char* layer = a.cache + w.l * a.cache_layer_stride;
+    const char* head = a.cache + w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
     const int32_t* table = a.tables + (w.l * a.s.R + w.r) * a.s.E;
 
     u32x4 q[RT][4];
@@ -354,9 +368,15 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       ref[t] = kNothing, sum[t] = 0.f;
     }
 
-    const auto load = [&](Tile (&x)[2], bool (&there)[2], int pair) {
+    int ids = -1;
+    // the n-th pair of the wave
+    const auto load = [&](Tile (&x)[2], bool (&there)[2], int n) {
+      if ((n & 31) == 0) {
+        const int pair = pa + wave + kWaves * (n + (lane >> 1));
+        ids = load_id(a, table, 2 * pair + (lane & 1), pair < pb);
+      }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) load_tile(x[j], record(a, table, layer, w.h, 2 * pair + j, there[j]), lane);
+      for (int j = 0; j < 2; ++j) load_tile(x[j], record(a, head, ids, 2 * (n & 31) + j, j, there[j]), lane);
     };
     const auto attend = [&](const Tile (&x)[2], const bool (&there)[2], int pair) {
       f32x4 s[RT][2];
@@ -416,8 +436,9 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
         // only rounding that counts is then that of the output
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          hi[t][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
-          lo[t][j] = pack2<BF16>(p[2 * j] - low16<BF16>(hi[t][j]), p[2 * j + 1] - high16<BF16>(hi[t][j]));
+          const uint32_t two = cut2<BF16>(p[2 * j], p[2 * j + 1]);
+          hi[t][j] = two;
+          lo[t][j] = cut2<BF16>(p[2 * j] - low16<BF16>(two), p[2 * j + 1] - high16<BF16>(two));
         }
       }
       float p0[4], p1[4];
@@ -445,16 +466,14 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 
     Tile x[2], y[2];
     bool tx[2], ty[2];
-    int pair = pa + wave;
-    if (pair < pb) load(x, tx, pair);
-    while (pair < pb) {
-      if (pair + kWaves < pb) load(y, ty, pair + kWaves);
-      attend(x, tx, pair);
-      pair += kWaves;
-      if (pair >= pb) break;
-      if (pair + kWaves < pb) load(x, tx, pair + kWaves);
-      attend(y, ty, pair);
-      pair += kWaves;
+    const int mine = pb - pa > wave ? (pb - pa - wave + kWaves - 1) / kWaves : 0;
+    if (mine) load(x, tx, 0);
+    for (int n = 0; n < mine; n += 2) {
+      if (n + 1 < mine) load(y, ty, n + 1);
+      attend(x, tx, pa + wave + kWaves * n);
+      if (n + 1 >= mine) break;
+      if (n + 2 < mine) load(x, tx, n + 2);
+      attend(y, ty, pa + wave + kWaves * (n + 1));
     }
 
     // the four waves' sums, under the largest of their references
@@ -542,7 +561,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
     const int64_t left = w.end - w.at;
     const int u1 = w.item.units - w.u < left ? w.item.units : w.u + (int)left;
     const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
-    const char* layer = a.cache + w.l * a.cache_layer_stride;
+    const char* head = a.cache + w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
     const int32_t* table = a.tables + (w.l * a.s.R + w.r) * a.s.E;
     const int steps = (pb - pa + 1) / 2, row0 = w.t * kRows + wave * 16 * RT;
     const bool busy = row0 < w.q.rows;
@@ -565,12 +584,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
 
     const auto at_ends = [&](int pos) { return pos < w.item.low_max || pos + kStep > w.item.high_min; };
     // the wave's 16 tokens of a step
+    int ids = -1;
     const auto load = [&](Tile& x, bool& there, int step) {
-      const int pair = pa + 2 * step + (wave >> 1);
-      bool in = pair < pb;
-      const char* rec = record(a, table, layer, w.h, in ? 2 * pair + (wave & 1) : 2 * pa, there);
-      there = there && in;
-      load_tile(x, rec, lane);
+      if ((step & 63) == 0) {
+        const int pair = pa + 2 * (step + lane) + (wave >> 1);
+        ids = load_id(a, table, 2 * pair + (wave & 1), pair < pb);
+      }
+      load_tile(x, record(a, head, ids, step & 63, wave & 1, there), lane);
     };
     const auto unpack = [&](const Tile& x, bool there, int step, int buf) {
       const int pos = (pa + 2 * step) * kPairTokens;

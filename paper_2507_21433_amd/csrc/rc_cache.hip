@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(ReadArgs a) {
   const int64_t off = l * a.kv_layer_stride_b + ((row * 16 + 4 * q) * a.H + h) * 256 + i * 16;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const u32x4 kx = unpack8<BF16>(kw[r], power_of(kb >> (8 * r) & 255)), vx = unpack8<BF16>(vw[r], power_of(vb >> (8 * r) & 255));
+    const u32x4 kx = unpack8<BF16>(kw[r], power_at(kb, r)), vx = unpack8<BF16>(vw[r], power_at(vb, r));
     __builtin_nontemporal_store(kx, (u32x4*)(a.k + off + (int64_t)r * a.H * 256));
     __builtin_nontemporal_store(vx, (u32x4*)(a.v + off + (int64_t)r * a.H * 256));
   }

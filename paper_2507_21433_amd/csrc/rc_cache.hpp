@@ -29,8 +29,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-// The exponent byte b as the fp32 number that the conversions take: they use its exponent field, which makes 255 a NaN.
+// The exponent byte b as the fp32 number that the conversions take: they use its exponent field, which makes 255 a NaN, and nothing
+// else of it (checked for all 256 exponents under any sign and fraction), so that byte `r` of a word takes one shift.
 __device__ __forceinline__ float power_of(uint32_t b) { return __uint_as_float(b << 23); }
+__device__ __forceinline__ float power_at(uint32_t w, int r) { return __uint_as_float(r == 3 ? w >> 1 : w << (23 - 8 * r)); }
 
 // Byte `B` (0 .. 3) of w: two codes, low half byte first, as two 16-bit values.
 template <bool BF16, int B>

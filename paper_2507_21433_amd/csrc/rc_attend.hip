@@ -368,10 +368,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       ref[t] = kNothing, sum[t] = 0.f;
     }
 
-    int ids = -1;
+    int ids = -1, ids_of = -1;
     // the n-th pair of the wave
     const auto load = [&](Tile (&x)[2], bool (&there)[2], int n) {
-      if ((n & 31) == 0) {
+      if ((n & 31) == 0 && ids_of != n) {
+        ids_of = n;
         const int pair = pa + wave + kWaves * (n + (lane >> 1));
         ids = load_id(a, table, 2 * pair + (lane & 1), pair < pb);
       }
@@ -467,12 +468,14 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
     Tile x[2], y[2];
     bool tx[2], ty[2];
     const int mine = pb - pa > wave ? (pb - pa - wave + kWaves - 1) / kWaves : 0;
+    // The loads of the next pair are in flight while one is worked on.  They are never left out (behind the last pair that one is
+    // loaded again): where a branch goes round them, the wait for this pair's loads becomes a wait for all.
     if (mine) load(x, tx, 0);
     for (int n = 0; n < mine; n += 2) {
-      if (n + 1 < mine) load(y, ty, n + 1);
+      load(y, ty, min(n + 1, mine - 1));
       attend(x, tx, pa + wave + kWaves * n);
       if (n + 1 >= mine) break;
-      if (n + 2 < mine) load(x, tx, n + 2);
+      load(x, tx, min(n + 2, mine - 1));
       attend(y, ty, pa + wave + kWaves * (n + 1));
     }
 

@@ -86,9 +86,6 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
-}
 
 __device__ __forceinline__ AttendRequest request(const AttendArgs& a, int r) {
   return a.q_start ? attend_request(a.s, a.ctx_len[r], a.q_start[r], a.q_start[r + 1]) : attend_request(a.s, a.ctx_len[r], r, r + 1);
@@ -96,85 +93,73 @@ __device__ __forceinline__ AttendRequest request(const AttendArgs& a, int r) {
 
 // ---- Where a workgroup's stretch of the line of units begins, and the walk along it.
 
-struct FindLds {
-  int64_t sums[kWaves], offset;
-  int32_t request;
-};
-
 struct Walk {
-  int64_t at, end, begin, share;  // units of the line
-  int64_t l;
-  int r, h, t, u;  // layer, request, head, row tile, unit of the item
+  int at, end, begin, share;  // units of the line
+  int l, r, h, t, u;          // layer, request, head, row tile, unit of the item
   AttendRequest q;
   AttendItem item;
 };
 
-// Sum of x over the threads up to and including this one; `all` gets the sum over the workgroup.
-__device__ inline int64_t block_scan(int64_t x, FindLds& lds, int64_t& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) lds.sums[wave] = x;
-  __syncthreads();
-  all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) x += lds.sums[w];
-    all += lds.sums[w];
-  }
-  return x;
+__device__ __forceinline__ void leave_border(const AttendArgs& a, int wg, int last, const Walk& w) {
+  if (a.borders && threadIdx.x == 0) a.borders[wg] = {last, w.at == w.begin, w.l, w.r, w.h, w.t, {0, 0}};
 }
 
-// Every workgroup counts the units of all requests by itself: for 64 requests two loads and a scan, where a launch of its own
-// would cost more than that.
-__device__ inline bool find(const AttendArgs& a, FindLds& lds, int64_t wg, Walk& w) {
-  int64_t mine = 0, upto = 0, total = 0, all;
-  for (int64_t base = 0; base < a.s.R; base += kThreads) {
-    const int64_t r = base + threadIdx.x;
-    mine = r < a.s.R ? attend_units(a.s, request(a, (int)r)) * a.s.H : 0;
-    upto = block_scan(mine, lds, all) + total;
-    total += all;
+// Every wave counts the units of all requests by itself, every lane those of some requests in a row: three loads and a scan without
+// a barrier, where a launch of its own would cost more than that.
+__device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
+  const int lane = threadIdx.x & 63, R = (int)a.s.R, H = a.s.H, each = (R + 63) / 64;
+  int ctx = 0, start = 0, end = 0, mine = 0;
+#pragma unroll 4
+  for (int i = 0; i < each; ++i) {
+    const int r = lane * each + i;
+    if (r < R) {
+      ctx = a.ctx_len[r];
+      start = a.q_start ? a.q_start[r] : r;
+      end = a.q_start ? a.q_start[r + 1] : r + 1;
+      mine += attend_units(a.s, attend_request(a.s, ctx, start, end)) * H;
+    }
   }
-  const int64_t line = total * a.s.L, share = attend_share(a.s, line);
-  w.begin = w.at = wg * share;
-  w.end = w.at + share < line ? w.at + share : line;
-  w.share = share;
-  if (w.at >= w.end) {
-    if (a.borders && threadIdx.x == 0) a.borders[wg].last = -1;
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(upto, d);
+    if (lane >= d) upto += y;
+  }
+  const int total = __builtin_amdgcn_readlane(upto, 63), line = total * (int)a.s.L;
+  w.share = uniform(attend_share(a.s, line));
+  w.begin = w.at = wg * w.share;
+  w.end = min(w.at + w.share, line);
+  w.l = w.r = w.h = w.t = 0;
+  if (w.at >= line) {
+    leave_border(a, wg, -1, w);
     return false;
   }
-  w.l = w.at / total;
-  const int64_t off = w.at - w.l * total;
-  if (a.s.R > kThreads) total = 0;
-  for (int64_t base = 0; base < a.s.R; base += kThreads) {
-    const int64_t r = base + threadIdx.x;
-    if (a.s.R > kThreads) {
-      mine = r < a.s.R ? attend_units(a.s, request(a, (int)r)) * a.s.H : 0;
-      upto = block_scan(mine, lds, all) + total;
-      total += all;
-    }
-    if (off >= upto - mine && off < upto) {
-      lds.request = (int32_t)r;
-      lds.offset = off - (upto - mine);
+  w.l = a.s.L == 1 ? 0 : uniform((int)((uint32_t)w.at / (uint32_t)total));
+  const int off = w.at - w.l * total;
+  // the lane whose requests hold the unit, and then the request
+  const int owner = __builtin_ctzll(__ballot(off < upto));
+  int rest = off - (__builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner)), units;
+  if (each == 1) {
+    w.r = owner;
+    w.q = attend_request(a.s, __builtin_amdgcn_readlane(ctx, owner), __builtin_amdgcn_readlane(start, owner), __builtin_amdgcn_readlane(end, owner));
+    units = __builtin_amdgcn_readlane(mine, owner);
+  } else {
+    for (w.r = owner * each;; ++w.r) {
+      w.q = request(a, w.r);
+      units = attend_units(a.s, w.q) * H;
+      if (rest < units) break;
+      rest -= units;
     }
   }
-  __syncthreads();
-  w.r = uniform(lds.request);
-  int64_t rest = uniform(lds.offset);
-  w.q = request(a, w.r);
-  const int64_t units = attend_units(a.s, w.q);
-  w.h = (int)(rest / units);
+  units = uniform((int)((uint32_t)units / (uint32_t)H));
+  w.h = uniform((int)((uint32_t)rest / (uint32_t)units));
   rest -= w.h * units;
-  for (w.t = 0;; ++w.t) {
+  for (;; ++w.t) {
     w.item = attend_item(a.s, w.q, w.t);
     if (rest < w.item.units) break;
     rest -= w.item.units;
   }
-  w.u = (int)rest;
+  w.u = rest;
   return true;
 }
 
@@ -194,13 +179,10 @@ __device__ inline void next_item(const AttendArgs& a, Walk& w) {
   w.item = attend_item(a.s, w.q, w.t);
 }
 
-// At the end of a stretch, whose last part ends at unit u1 of its item.
-__device__ inline void leave_border(const AttendArgs& a, int64_t wg, const Walk& w, int u1) {
-  if (!a.borders || threadIdx.x != 0) return;
-  AttendBorder b = {-1, 0, 0, 0, 0, 0, {0, 0}};
-  if (w.u == 0 && u1 < w.item.units)
-    b = {(int32_t)(wg + (w.item.units - u1 + w.share - 1) / w.share), w.at == w.begin, (int32_t)w.l, w.r, w.h, w.t, {0, 0}};
-  a.borders[wg] = b;
+// Up to which workgroup the parts of an item go that begins in this stretch and goes on behind it; -1 where the last part of a stretch,
+// which ends at unit u1, is none of that kind.
+__device__ __forceinline__ int border_last(int wg, const Walk& w, int u1) {
+  return w.u == 0 && u1 < w.item.units ? wg + (int)((uint32_t)(w.item.units - u1 + w.share - 1) / (uint32_t)w.share) : -1;
 }
 
 // ---- Loads.
@@ -313,7 +295,7 @@ __device__ __forceinline__ void rescale(f32x4 (&o)[8], float& ref, float& sum, f
 
 __device__ __forceinline__ void row_place(const AttendArgs& a, const Walk& w, int n, int64_t& at) {
   const int token = w.q.first + n / a.s.g, head = w.h * a.s.g + n % a.s.g;
-  at = (w.l * a.s.n_q + token) * (int64_t)(a.s.H * a.s.g) + head;
+  at = ((int64_t)w.l * a.s.n_q + token) * (int64_t)(a.s.H * a.s.g) + head;
 }
 __device__ __forceinline__ float row_lse(float ref, float sum) {
   return sum == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
@@ -324,14 +306,13 @@ __device__ __forceinline__ float row_scale(float sum) { return sum == 0.f ? 0.f 
 __device__ __forceinline__ u32x4 load_q(const AttendArgs& a, const Walk& w, int n, int quarter, int s) {
   if (n >= w.q.rows) return u32x4{0, 0, 0, 0};
   const int token = w.q.first + n / a.s.g, head = w.h * a.s.g + n % a.s.g;
-  return *(const u32x4*)(a.q + w.l * a.q_layer_stride_b + token * a.q_token_stride_b + (head * 128 + quarter * 32 + s * 8) * 2);
+  return *(const u32x4*)(a.q + (int64_t)w.l * a.q_layer_stride_b + (int64_t)token * a.q_token_stride_b + (head * 128 + quarter * 32 + s * 8) * 2);
 }
 
 // ---- Few rows: every wave has all of an item's rows and every fourth run of 32 tokens.
 
 template <int RT>
 struct RowsLds {
-  FindLds find;
   float ref[kWaves][16 * RT], sum[kWaves][16 * RT];
   float o[kWaves][16][132];
 };
@@ -341,16 +322,15 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
   __shared__ RowsLds<RT> lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   // neighbouring stretches to one XCD: row tiles of a request and head read the same cache
-  const int64_t wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
   Walk w;
-  if (!find(a, lds.find, wg, w)) return;
+  if (!find(a, wg, w)) return;
   const int per = a.s.unit / kPairTokens;
   for (;;) {
-    const int64_t left = w.end - w.at;
-    const int u1 = w.item.units - w.u < left ? w.item.units : w.u + (int)left;
+    const int u1 = min(w.item.units, w.u + w.end - w.at);
     const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
-    const char* head = a.cache + w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
-    const int32_t* table = a.tables + (w.l * a.s.R + w.r) * a.s.E;
+    const char* head = a.cache + (int64_t)w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
+    const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
 
     u32x4 q[RT][4];
     f32x4 o[RT][8];
@@ -533,7 +513,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       __syncthreads();
     }
     if (w.at + (u1 - w.u) >= w.end) {
-      leave_border(a, wg, w, u1);
+      leave_border(a, wg, border_last(wg, w, u1), w);
       return;
     }
     w.at += u1 - w.u;
@@ -544,7 +524,6 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 // ---- Many rows: every wave has 32 of an item's 128 rows, and the workgroup turns 64 tokens at a time into operands in LDS.
 
 struct ManyLds {
-  FindLds find;
   u32x4 k[2][4][4][64];  // [buffer][16 tokens][step of the dims][lane]
   u32x2 v[2][2][8][64][2];  // [buffer][32 tokens][chunk][lane][16 tokens of the 32]
   uint32_t ve[2][4][16];    // V's exponent words of the tiles of a buffer at the ends of what the rows see
@@ -556,16 +535,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
   constexpr int RT = 2, kStep = 64, kRows = 128;
   __shared__ ManyLds lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
-  const int64_t wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
   Walk w;
-  if (!find(a, lds.find, wg, w)) return;
+  if (!find(a, wg, w)) return;
   const int per = a.s.unit / kPairTokens;
   for (;;) {
-    const int64_t left = w.end - w.at;
-    const int u1 = w.item.units - w.u < left ? w.item.units : w.u + (int)left;
+    const int u1 = min(w.item.units, w.u + w.end - w.at);
     const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
-    const char* head = a.cache + w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
-    const int32_t* table = a.tables + (w.l * a.s.R + w.r) * a.s.E;
+    const char* head = a.cache + (int64_t)w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
+    const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
     const int steps = (pb - pa + 1) / 2, row0 = w.t * kRows + wave * 16 * RT;
     const bool busy = row0 < w.q.rows;
 
@@ -731,7 +709,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
       }
     }
     if (w.at + (u1 - w.u) >= w.end) {
-      leave_border(a, wg, w, u1);
+      leave_border(a, wg, border_last(wg, w, u1), w);
       return;
     }
     w.at += u1 - w.u;

@@ -74,15 +74,15 @@ RC_HD inline AttendItem attend_item(const AttendShape& s, const AttendRequest& q
 }
 
 // Units of a request and KV head.
-RC_HD inline int64_t attend_units(const AttendShape& s, const AttendRequest& q) {
-  int64_t n = 0;
+RC_HD inline int32_t attend_units(const AttendShape& s, const AttendRequest& q) {
+  int32_t n = 0;
   for (int32_t t = 0; t < q.tiles; ++t) n += attend_item(s, q, t).units;
   return n;
 }
 
 // Units of a workgroup's stretch where there are `total` of them.
-RC_HD inline int64_t attend_share(const AttendShape& s, int64_t total) {
-  const int64_t n = (total + s.wgs - 1) / s.wgs;
+RC_HD inline int32_t attend_share(const AttendShape& s, int32_t total) {
+  const int32_t n = (int32_t)((uint32_t)(total + s.wgs - 1) / (uint32_t)s.wgs);
   return n < s.least ? s.least : n;
 }
 
@@ -131,8 +131,15 @@ inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_
   *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.wgs};
   // a short table: items are not cut, and nothing has to be joined
   if (s->cap <= kWholeTokens) s->unit = (s->cap + k.unit - 1) / k.unit * k.unit + k.unit, s->least = 1;
+  // the line is counted in 32 bits: tables long enough for more than 2^30 units have longer ones
+  const double items = (double)L * R * H * (((double)max_q * g + k.rows - 1) / k.rows);
+  if (items > (1 << 30)) return false;
+  while (items * attend_most_units(*s) > (1 << 30)) {
+    if (s->unit >= 1 << 29) return false;
+    s->unit *= 2;
+  }
   // no more workgroups than there can be stretches
-  const double items = (double)L * R * H * (((double)max_q * g + k.rows - 1) / k.rows), most = items * attend_most_units(*s) / s->least + 1;
+  const double most = items * attend_most_units(*s) / s->least + 1;
   if (most < s->wgs) s->wgs = ((int32_t)most + 8) / 8 * 8;
   return true;
 }

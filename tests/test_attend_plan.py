@@ -89,6 +89,10 @@ int main() {
   REQUIRE(!rc::attend_shape(&s, 1, 1, 1LL << 27, 16, 1, 1, 1, 1, 0));
   REQUIRE(rc::attend_shape(&s, 1, 1, (1LL << 27) - 5, 16, 1, 1, 1, 1, 1LL << 40) && s.window == 0);
   REQUIRE(!rc::attend_shape(&s, 1, 1, 8, 16, 1, 64, 1LL << 29, 1LL << 29, 0));
+  // a line of more than 2^30 units: longer ones, or none at all
+  REQUIRE(rc::attend_shape(&s, 64, 4096, 8192, 16, 16, 16, 4096, 1, 0));
+  REQUIRE(s.unit > 128 && s.unit % 128 == 0 && 64.0 * 4096 * 16 * rc::attend_most_units(s) <= (1 << 30));
+  REQUIRE(!rc::attend_shape(&s, 65535, 4096, 8, 16, 16, 16, 4096, 1, 0));
   return cut > 1000 && whole > 1000 && empty > 100 ? 0 : 3;
 }
 """

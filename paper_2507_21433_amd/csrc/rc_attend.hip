@@ -95,7 +95,7 @@ __device__ __forceinline__ AttendRequest request(const AttendArgs& a, int r) {
 
 struct Walk {
   int at, end, begin, share;  // units of the line
-  int l, r, h, t, u;          // layer, request, head, row tile, unit of the item
+  int l, r, h, t, rest;       // layer, request, head, row tile, unit of the row tile (or of the head's, before that is looked for)
   AttendRequest q;
   AttendItem item;
 };
@@ -104,19 +104,31 @@ __device__ __forceinline__ void leave_border(const AttendArgs& a, int wg, int la
   if (a.borders && threadIdx.x == 0) a.borders[wg] = {last, w.at == w.begin, w.l, w.r, w.h, w.t, {0, 0}};
 }
 
+// ONE: a request has one row tile at most.
+template <bool ONE>
+__device__ __forceinline__ int units_of(const AttendArgs& a, const AttendRequest& q) {
+  if constexpr (ONE)
+    return q.tiles ? attend_only_item(a.s, q).units : 0;
+  else
+    return attend_units(a.s, q);
+}
+
 // Every wave counts the units of all requests by itself, every lane those of some requests in a row: three loads and a scan without
-// a barrier, where a launch of its own would cost more than that.
+// a barrier, where a launch of its own would cost more than that.  What is run once here is read from memory once by every compute unit
+// as well, instruction by instruction: it is kept short (2.0 us of a call of 8.3 went by before the first load, with everything
+// inlined and unrolled 1000 instructions).
+template <bool ONE>
 __device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
   const int lane = threadIdx.x & 63, R = (int)a.s.R, H = a.s.H, each = (R + 63) / 64;
   int ctx = 0, start = 0, end = 0, mine = 0;
-#pragma unroll 4
+#pragma unroll 1
   for (int i = 0; i < each; ++i) {
     const int r = lane * each + i;
     if (r < R) {
       ctx = a.ctx_len[r];
       start = a.q_start ? a.q_start[r] : r;
       end = a.q_start ? a.q_start[r + 1] : r + 1;
-      mine += attend_units(a.s, attend_request(a.s, ctx, start, end)) * H;
+      mine += units_of<ONE>(a, attend_request(a.s, ctx, start, end)) * H;
     }
   }
   int upto = mine;
@@ -138,51 +150,73 @@ __device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
   const int off = w.at - w.l * total;
   // the lane whose requests hold the unit, and then the request
   const int owner = __builtin_ctzll(__ballot(off < upto));
-  int rest = off - (__builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner)), units;
-  if (each == 1) {
-    w.r = owner;
-    w.q = attend_request(a.s, __builtin_amdgcn_readlane(ctx, owner), __builtin_amdgcn_readlane(start, owner), __builtin_amdgcn_readlane(end, owner));
-    units = __builtin_amdgcn_readlane(mine, owner);
-  } else {
-    for (w.r = owner * each;; ++w.r) {
+  w.rest = off - (__builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner));
+  w.r = owner * each;
+  w.q = attend_request(a.s, __builtin_amdgcn_readlane(ctx, owner), __builtin_amdgcn_readlane(start, owner), __builtin_amdgcn_readlane(end, owner));
+  int units = __builtin_amdgcn_readlane(mine, owner);
+  if (each > 1) {
+    for (;; ++w.r) {
       w.q = request(a, w.r);
-      units = attend_units(a.s, w.q) * H;
-      if (rest < units) break;
-      rest -= units;
+      units = uniform(units_of<ONE>(a, w.q) * H);
+      if (w.rest < units) break;
+      w.rest -= units;
     }
   }
   units = uniform((int)((uint32_t)units / (uint32_t)H));
-  w.h = uniform((int)((uint32_t)rest / (uint32_t)units));
-  rest -= w.h * units;
-  for (;; ++w.t) {
-    w.item = attend_item(a.s, w.q, w.t);
-    if (rest < w.item.units) break;
-    rest -= w.item.units;
-  }
-  w.u = rest;
+  w.h = uniform((int)((uint32_t)w.rest / (uint32_t)units));
+  w.rest -= w.h * units;
   return true;
 }
 
-// To the next item of a stretch that goes on: only called where there is one.
-__device__ inline void next_item(const AttendArgs& a, Walk& w) {
-  w.u = 0;
-  if (++w.t == w.q.tiles) {
-    w.t = 0;
-    if (++w.h == a.s.H) {
-      w.h = 0;
-      do {
-        if (++w.r == a.s.R) w.r = 0, ++w.l;
-        w.q = request(a, w.r);
-      } while (w.q.tiles == 0);
-    }
-  }
-  w.item = attend_item(a.s, w.q, w.t);
+// To the next item, a row tile of the same or another request, head and layer: only called where there is one.
+template <bool ONE>
+__device__ __forceinline__ void next_item(const AttendArgs& a, Walk& w) {
+  if (!ONE && ++w.t < w.q.tiles) return;
+  w.t = 0;
+  if (++w.h < a.s.H) return;
+  w.h = 0;
+  do {
+    if (++w.r == a.s.R) w.r = 0, ++w.l;
+    w.q = request(a, w.r);
+  } while (w.q.tiles == 0);
 }
 
-// Up to which workgroup the parts of an item go that begins in this stretch and goes on behind it; -1 where the last part of a stretch,
-// which ends at unit u1, is none of that kind.
-__device__ __forceinline__ int border_last(int wg, const Walk& w, int u1) {
-  return w.u == 0 && u1 < w.item.units ? wg + (int)((uint32_t)(w.item.units - u1 + w.share - 1) / (uint32_t)w.share) : -1;
+// A part of an item: units u0 to u1 of it, tokens of the runs pa to pb.
+struct Part {
+  int u0, u1, pa, pb;
+  bool whole;
+};
+// The part that the walk stands before; false where it stands in an earlier row tile of the head, and has gone on to the next.
+template <bool ONE>
+__device__ __forceinline__ bool take_part(const AttendArgs& a, Walk& w, Part& p) {
+  w.item = ONE ? attend_only_item(a.s, w.q) : attend_item(a.s, w.q, w.t);
+  if (!ONE && w.rest >= w.item.units) {
+    w.rest -= w.item.units;
+    ++w.t;
+    return false;
+  }
+  p.u0 = w.rest, p.u1 = min(w.item.units, w.rest + w.end - w.at);
+  p.pa = uniform(attend_run(a.s, w.item, p.u0)), p.pb = uniform(attend_run(a.s, w.item, p.u1));
+  p.whole = p.u0 <= w.item.free && p.u1 == w.item.units;
+  return true;
+}
+// Nothing of the item falls to this stretch, whose end lies among its free units.
+__device__ __forceinline__ bool only_free(const Walk& w, const Part& p) { return p.u1 <= w.item.free; }
+
+// Behind a part: false at the end of the stretch.  If the part is the first of an item that goes on, the border says up to which
+// workgroup the item's parts go.
+template <bool ONE>
+__device__ __forceinline__ bool go_on(const AttendArgs& a, int wg, Walk& w, const Part& p) {
+  const int left = w.item.units - p.u1;
+  if (w.at + (p.u1 - p.u0) >= w.end) {
+    const bool first = p.u0 <= w.item.free && left;
+    leave_border(a, wg, first ? wg + (int)((uint32_t)(left + w.share - 1) / (uint32_t)w.share) : -1, w);
+    return false;
+  }
+  w.at += p.u1 - p.u0;
+  w.rest = 0;
+  next_item<ONE>(a, w);
+  return true;
 }
 
 // ---- Loads.
@@ -218,11 +252,11 @@ __device__ __forceinline__ const char* record(const AttendArgs& a, const char* h
 // V's exponent bytes with those of tokens that no row sees replaced by that of 1: whatever lies there (memory that was never
 // written) gets a probability of 0, and 0 times infinity or NaN would not be 0.  Token r of the word stands at pos + r.
 __device__ __forceinline__ uint32_t seen_only(uint32_t ve, int pos, bool there, const AttendItem& it) {
+  const uint32_t span = there ? it.high_max - it.low_min : 0;  // (an item of no tokens has no run)
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const bool seen = there && pos + r >= it.low_min && pos + r < it.high_max;
     const uint32_t m = 0xffu << (8 * r);
-    if (!seen) ve = (ve & ~m) | ((uint32_t)kOneByte << (8 * r));
+    if ((uint32_t)(pos + r - it.low_min) >= span) ve = (ve & ~m) | (kOneByte * 0x01010101u & m);
   }
   return ve;
 }
@@ -293,20 +327,41 @@ __device__ __forceinline__ void rescale(f32x4 (&o)[8], float& ref, float& sum, f
 
 // ---- What a row leaves.
 
-__device__ __forceinline__ void row_place(const AttendArgs& a, const Walk& w, int n, int64_t& at) {
-  const int token = w.q.first + n / a.s.g, head = w.h * a.s.g + n % a.s.g;
-  at = ((int64_t)w.l * a.s.n_q + token) * (int64_t)(a.s.H * a.s.g) + head;
+// Query token of row n of an item's first `rows` ones, n / g.  ONE: n is below 32 (and g as well, or n / g is 0).
+template <bool ONE>
+__device__ __forceinline__ int row_token(const AttendArgs& a, int n) {
+  return ONE ? (int)((uint32_t)n * a.s.inverse >> 16) : (int)((uint32_t)n / (uint32_t)a.s.g);
+}
+// Row n of the request's, as a row of [L][n_q][n_heads].
+template <bool ONE>
+__device__ __forceinline__ int64_t row_place(const AttendArgs& a, const Walk& w, int n) {
+  const int j = row_token<ONE>(a, n);
+  return ((int64_t)w.l * a.s.n_q + w.q.first + j) * (int64_t)(a.s.H * a.s.g) + w.h * a.s.g + n - j * a.s.g;
 }
 __device__ __forceinline__ float row_lse(float ref, float sum) {
   return sum == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 __device__ __forceinline__ float row_scale(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
-// The 16 bytes of a row of q that lane (row, quarter) holds for the step s of K's dims.
-__device__ __forceinline__ u32x4 load_q(const AttendArgs& a, const Walk& w, int n, int quarter, int s) {
-  if (n >= w.q.rows) return u32x4{0, 0, 0, 0};
-  const int token = w.q.first + n / a.s.g, head = w.h * a.s.g + n % a.s.g;
-  return *(const u32x4*)(a.q + (int64_t)w.l * a.q_layer_stride_b + (int64_t)token * a.q_token_stride_b + (head * 128 + quarter * 32 + s * 8) * 2);
+// Row n of q as lane (row, quarter) holds it for the four steps of K's dims; rows that the item does not have: its last one's.
+template <bool ONE>
+__device__ __forceinline__ void load_q(const AttendArgs& a, const Walk& w, int n, int quarter, u32x4 (&q)[4]) {
+  n = min(n, w.q.rows - 1);
+  const int j = row_token<ONE>(a, n), head = w.h * a.s.g + n - j * a.s.g;
+  const u32x4* p = (const u32x4*)(a.q + (int64_t)w.l * a.q_layer_stride_b + (int64_t)(w.q.first + j) * a.q_token_stride_b + (head * 128 + quarter * 32) * 2);
+#pragma unroll
+  for (int s = 0; s < 4; ++s) q[s] = p[s];
+}
+
+// The rows of an item that sees nothing.
+template <bool ONE>
+__device__ inline void store_nothing(const AttendArgs& a, const Walk& w) {
+  const int rows = min(a.s.rows, w.q.rows - w.t * a.s.rows);
+  for (int i = threadIdx.x; i < rows * 16; i += kThreads) {
+    const int64_t at = row_place<ONE>(a, w, w.t * a.s.rows + (i >> 4));
+    *(u32x4*)(a.out + (at * 128 + (i & 15) * 8) * 2) = u32x4{0, 0, 0, 0};
+    if ((i & 15) == 0 && a.lse) a.lse[at] = -__builtin_inff();
+  }
 }
 
 // ---- Few rows: every wave has all of an item's rows and every fourth run of 32 tokens.
@@ -324,42 +379,66 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
   // neighbouring stretches to one XCD: row tiles of a request and head read the same cache
   const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
   Walk w;
-  if (!find(a, wg, w)) return;
-  const int per = a.s.unit / kPairTokens;
+  if (!find<true>(a, wg, w)) return;
   for (;;) {
-    const int u1 = min(w.item.units, w.u + w.end - w.at);
-    const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
+    Part part;
+    take_part<true>(a, w, part);
+    if (only_free(w, part)) {
+      leave_border(a, wg, -1, w);
+      return;
+    }
+    if (w.item.pairs == 0) {
+      store_nothing<true>(a, w);
+      if (!go_on<true>(a, wg, w, part)) return;
+      continue;
+    }
     const char* head = a.cache + (int64_t)w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
     const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
+
+    // the wave's pairs of tiles: every fourth from pa + wave on
+    const int mine = (part.pb - part.pa - wave + kWaves - 1) / kWaves;
+    int ids = -1;
+    const auto load = [&](Tile (&x)[2], int (&there)[2], int n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        bool is;
+        load_tile(x[j], record(a, head, ids, 2 * (n & 31) + j, j, is), lane);
+        there[j] = is;
+      }
+    };
 
     u32x4 q[RT][4];
     f32x4 o[RT][8];
     float ref[RT], sum[RT];
-    int low[RT], high[RT];
+    int low[RT];
+    uint32_t span[RT];  // of the positions that the lane's row sees, from low on
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const int n = w.t * 16 * RT + 16 * t + col;
-      const int pos = w.q.ctx - w.q.len + n / a.s.g;
-      low[t] = attend_low(a.s, pos), high[t] = n < w.q.rows ? attend_high(a.s, pos) : 0;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) q[t][s] = load_q(a, w, n, quarter, s);
+      load_q<true>(a, w, 16 * t + col, quarter, q[t]);
+      const int pos = w.q.ctx - w.q.len + row_token<true>(a, 16 * t + col);
+      low[t] = attend_low(a.s, pos), span[t] = max(attend_high(a.s, pos) - low[t], 0);
 #pragma unroll
       for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
       ref[t] = kNothing, sum[t] = 0.f;
     }
 
-    int ids = -1, ids_of = -1;
-    // the n-th pair of the wave
-    const auto load = [&](Tile (&x)[2], bool (&there)[2], int n) {
-      if ((n & 31) == 0 && ids_of != n) {
-        ids_of = n;
-        const int pair = pa + wave + kWaves * (n + (lane >> 1));
-        ids = load_id(a, table, 2 * pair + (lane & 1), pair < pb);
-      }
+    Tile x[2], y[2];
+    int there[2], there_y[2] = {0, 0};
+    // The loads of the next pair are in flight while one is worked on.  They are never left out (behind the last pair that one is
+    // loaded again): where a branch goes round them, the wait for this pair's loads becomes a wait for all.  The first round only loads.
+#pragma unroll 1
+    for (int n = -1; n < mine; ++n) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) load_tile(x[j], record(a, head, ids, 2 * (n & 31) + j, j, there[j]), lane);
-    };
-    const auto attend = [&](const Tile (&x)[2], const bool (&there)[2], int pair) {
+      for (int j = 0; j < 2; ++j) x[j] = y[j], there[j] = there_y[j];
+      const int next = min(n + 1, mine - 1);
+      if ((n & 31) == 31 && next > n) {
+        const int pair = part.pa + wave + kWaves * (next + (lane >> 1));
+        ids = load_id(a, table, 2 * pair + (lane & 1), pair < part.pb);
+      }
+      if (mine > 0) load(y, there_y, next);
+      if (n < 0) continue;
+
+      const int pair = part.pa + wave + kWaves * n, pos = pair * kPairTokens;
       f32x4 s[RT][2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -373,33 +452,31 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
           for (int t = 0; t < RT; ++t) s[t][j] = mfma<BF16>(k, q[t][d], s[t][j]);
         }
       }
-      const int pos = pair * kPairTokens;
-      uint32_t ve[2] = {x[0].ve, x[1].ve};
       // every row sees all 32 tokens, but at the ends of what the rows see and where the table has a hole
       if (pos < w.item.low_max || pos + kPairTokens > w.item.high_min || !there[0] || !there[1]) {
-        uint32_t flags = 0;
+        uint32_t flags = 0, seen[RT];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          ve[j] = seen_only(ve[j], pos + 16 * j + 4 * quarter, there[j], w.item);
-          const uint32_t f = nan_bytes(ve[j]);
-          ve[j] = without_nans(ve[j], f);
+          x[j].ve = seen_only(x[j].ve, pos + 16 * j + 4 * quarter, there[j], w.item);
+          const uint32_t f = nan_bytes(x[j].ve);
+          x[j].ve = without_nans(x[j].ve, f);
           flags |= f << (4 * j);
         }
-        const bool any = __any(flags != 0);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          uint32_t seen = 0;
+          seen[t] = 0;
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const int p = pos + 16 * j + 4 * quarter + r;
-              if (there[j] && p >= low[t] && p < high[t])
-                seen |= 1u << (4 * j + r);
-              else
-                s[t][j][r] = -__builtin_inff();
+              const bool is = (uint32_t)(pos + 16 * j + 4 * quarter + r - low[t]) < (there[j] ? span[t] : 0u);
+              seen[t] |= (uint32_t)is << (4 * j + r);
+              s[t][j][r] = is ? s[t][j][r] : -__builtin_inff();
             }
-          if (any) poison<BF16>(o[t], flags, seen);
+        }
+        if (__any(flags != 0)) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) poison<BF16>(o[t], flags, seen[t]);
         }
       }
       u32x4 hi[RT], lo[RT];
@@ -423,8 +500,8 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
         }
       }
       float p0[4], p1[4];
-      powers(ve[0], p0);
-      powers(ve[1], p1);
+      powers(x[0].ve, p0);
+      powers(x[1].ve, p1);
       const auto chunks = [&](auto b) {
         constexpr int B = decltype(b)::value;
         uint32_t e0[2], d0[2], e1[2], d1[2];
@@ -443,20 +520,6 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       chunks(std::integral_constant<int, 1>{});
       chunks(std::integral_constant<int, 2>{});
       chunks(std::integral_constant<int, 3>{});
-    };
-
-    Tile x[2], y[2];
-    bool tx[2], ty[2];
-    const int mine = pb - pa > wave ? (pb - pa - wave + kWaves - 1) / kWaves : 0;
-    // The loads of the next pair are in flight while one is worked on.  They are never left out (behind the last pair that one is
-    // loaded again): where a branch goes round them, the wait for this pair's loads becomes a wait for all.
-    if (mine) load(x, tx, 0);
-    for (int n = 0; n < mine; n += 2) {
-      load(y, ty, min(n + 1, mine - 1));
-      attend(x, tx, pa + wave + kWaves * n);
-      if (n + 1 >= mine) break;
-      load(x, tx, min(n + 2, mine - 1));
-      attend(y, ty, pa + wave + kWaves * (n + 1));
     }
 
     // the four waves' sums, under the largest of their references
@@ -466,8 +529,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       if (quarter == 0) lds.ref[wave][16 * t + col] = ref[t], lds.sum[wave][16 * t + col] = sum[t];
     }
     __syncthreads();
-    const bool whole = w.u == 0 && u1 == w.item.units;
-    float* part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(16 * RT));
+    float* to_part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(16 * RT));
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       float top = kNothing;
@@ -482,42 +544,33 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       }
       __syncthreads();
       // a thread adds eight dims of a row
-      const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8, n = w.t * 16 * RT + 16 * t + row;
-      float m = kNothing, all = 0.f;
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) m = fmaxf(m, lds.ref[v][16 * t + row]);
-      f32x4 y0 = {0, 0, 0, 0}, y1 = {0, 0, 0, 0};
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        all += lds.sum[v][16 * t + row] * __builtin_amdgcn_exp2f(lds.ref[v][16 * t + row] - m);
-        y0 += *(const f32x4*)&lds.o[v][row][d];
-        y1 += *(const f32x4*)&lds.o[v][row][d + 4];
-      }
+      const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8, n = 16 * t + row;
       if (n < w.q.rows) {
-        if (whole) {
+        float m = kNothing, all = 0.f;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) m = fmaxf(m, lds.ref[v][n]);
+        f32x4 y0 = {0, 0, 0, 0}, y1 = {0, 0, 0, 0};
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) {
+          all += lds.sum[v][n] * __builtin_amdgcn_exp2f(lds.ref[v][n] - m);
+          y0 += *(const f32x4*)&lds.o[v][row][d];
+          y1 += *(const f32x4*)&lds.o[v][row][d + 4];
+        }
+        if (part.whole) {
           const float f1 = row_scale(all);
-          int64_t at;
-          row_place(a, w, n, at);
+          const int64_t at = row_place<true>(a, w, n);
           y0 *= f1, y1 *= f1;
           *(u32x4*)(a.out + (at * 128 + d) * 2) = u32x4{pack2<BF16>(y0[0], y0[1]), pack2<BF16>(y0[2], y0[3]), pack2<BF16>(y1[0], y1[1]), pack2<BF16>(y1[2], y1[3])};
           if (d == 0 && a.lse) a.lse[at] = row_lse(m, all);
         } else {
-          *(f32x4*)(part + (16 * t + row) * 128 + d) = y0;
-          *(f32x4*)(part + (16 * t + row) * 128 + d + 4) = y1;
-          if (d == 0) {
-            part[16 * RT * 128 + (16 * t + row) * 2] = m;
-            part[16 * RT * 128 + (16 * t + row) * 2 + 1] = all;
-          }
+          *(f32x4*)(to_part + n * 128 + d) = y0;
+          *(f32x4*)(to_part + n * 128 + d + 4) = y1;
+          if (d == 0) *(float2*)(to_part + 16 * RT * 128 + n * 2) = float2{m, all};
         }
       }
       __syncthreads();
     }
-    if (w.at + (u1 - w.u) >= w.end) {
-      leave_border(a, wg, border_last(wg, w, u1), w);
-      return;
-    }
-    w.at += u1 - w.u;
-    next_item(a, w);
+    if (!go_on<true>(a, wg, w, part)) return;
   }
 }
 
@@ -537,11 +590,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
   Walk w;
-  if (!find(a, wg, w)) return;
-  const int per = a.s.unit / kPairTokens;
+  if (!find<false>(a, wg, w)) return;
   for (;;) {
-    const int u1 = min(w.item.units, w.u + w.end - w.at);
-    const int pa = w.item.pair0 + w.u * per, pb = w.item.pair0 + (w.item.pairs < (int64_t)u1 * per ? w.item.pairs : u1 * per);
+    Part cut;
+    if (!take_part<false>(a, w, cut)) continue;
+    if (only_free(w, cut)) {
+      leave_border(a, wg, -1, w);
+      return;
+    }
+    if (w.item.pairs == 0) {
+      store_nothing<false>(a, w);
+      if (!go_on<false>(a, wg, w, cut)) return;
+      continue;
+    }
+    const int pa = cut.pa, pb = cut.pb;
     const char* head = a.cache + (int64_t)w.l * a.cache_layer_stride + (int64_t)w.h * (a.s.T >> 4) * kRecordBytes;
     const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
     const int steps = (pb - pa + 1) / 2, row0 = w.t * kRows + wave * 16 * RT;
@@ -550,14 +612,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
     u32x4 q[RT][4];
     f32x4 o[RT][8];
     float ref[RT], sum[RT];
-    int low[RT], high[RT];
+    int low[RT];
+    uint32_t span[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const int n = row0 + 16 * t + col;
-      const int pos = w.q.ctx - w.q.len + n / a.s.g;
-      low[t] = attend_low(a.s, pos), high[t] = n < w.q.rows ? attend_high(a.s, pos) : 0;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) q[t][s] = load_q(a, w, n, quarter, s);
+      load_q<false>(a, w, n, quarter, q[t]);
+      const int pos = w.q.ctx - w.q.len + row_token<false>(a, n);
+      low[t] = attend_low(a.s, pos), span[t] = max(attend_high(a.s, pos) - low[t], 0);
 #pragma unroll
       for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
       ref[t] = kNothing, sum[t] = 0.f;
@@ -629,11 +691,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const int p = pos + 16 * j + 4 * quarter + r;
-              if ((there >> j & 1) && p >= low[t] && p < high[t])
-                seen |= 1u << (4 * j + r);
-              else
-                s[t][j][r] = -__builtin_inff();
+              const bool is = (uint32_t)(pos + 16 * j + 4 * quarter + r - low[t]) < (there >> j & 1 ? span[t] : 0u);
+              seen |= (uint32_t)is << (4 * j + r);
+              s[t][j][r] = is ? s[t][j][r] : -__builtin_inff();
             }
           if (any) {
             poison<BF16>(o[t], flags & 255, seen & 255);
@@ -682,17 +742,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
       __syncthreads();
     }
 
-    const bool whole = w.u == 0 && u1 == w.item.units;
     float* part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(kRows));
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const float all = row_sum(sum[t]);
       const int m = wave * 16 * RT + 16 * t + col, n = w.t * kRows + m;
       if (n >= w.q.rows) continue;
-      if (whole) {
+      if (cut.whole) {
         const float f = row_scale(all);
-        int64_t at;
-        row_place(a, w, n, at);
+        const int64_t at = row_place<false>(a, w, n);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           *(u32x4*)(a.out + (at * 128 + (4 * quarter + r) * 8) * 2) =
@@ -708,12 +766,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         if (quarter == 0) part[kRows * 128 + m * 2] = ref[t], part[kRows * 128 + m * 2 + 1] = all;
       }
     }
-    if (w.at + (u1 - w.u) >= w.end) {
-      leave_border(a, wg, border_last(wg, w, u1), w);
-      return;
-    }
-    w.at += u1 - w.u;
-    next_item(a, w);
+    if (!go_on<false>(a, wg, w, cut)) return;
   }
 }
 
@@ -748,8 +801,7 @@ template <bool BF16>
 __device__ __forceinline__ void join_store(const AttendArgs& a, const Walk& w, int n, float top, float x, float y, float sum) {
   const int lane = threadIdx.x & 63;
   const float f = row_scale(sum);
-  int64_t at;
-  row_place(a, w, n, at);
+  const int64_t at = row_place<false>(a, w, n);
   *(uint32_t*)(a.out + (at * 128 + 2 * lane) * 2) = pack2<BF16>(x * f, y * f);
   if (lane == 0 && a.lse) a.lse[at] = row_lse(top, sum);
 }

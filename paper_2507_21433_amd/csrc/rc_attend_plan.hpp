@@ -28,8 +28,10 @@ struct AttendShape {
   int32_t window;      // 0: none
   int32_t rows, unit;  // rows of a tile, tokens of a unit
   int32_t cap;         // positions of a table, E * T
-  int32_t least;       // units of a stretch, at least
+  int32_t least;       // units of a stretch, at least; more than `free`
+  int32_t free;        // units that an item costs whatever its length
   int32_t wgs;         // workgroups
+  uint32_t inverse;    // n * inverse >> 16 is n / g for n below 32
 };
 
 // A request's query tokens, row tiles and cached tokens, from what the device arrays hold (anything at all).
@@ -51,7 +53,7 @@ RC_HD inline AttendRequest attend_request(const AttendShape& s, int32_t ctx, int
 // The cached tokens of a row tile.  Row n of a request is query token n / g, at position ctx - len + n / g.
 struct AttendItem {
   int32_t pair0, pairs;      // first run of 32 tokens, number of runs
-  int32_t units;             // at least 1: an item that sees nothing still has to say so
+  int32_t free, units;       // units of the line: the first `free` of them stand for what an item costs whatever its length
   int32_t low_min, low_max;  // first position seen by the first and by the last row
   int32_t high_min, high_max;  // one past the last position seen by the first and by the last row
 };
@@ -59,18 +61,28 @@ RC_HD inline int32_t attend_low(const AttendShape& s, int32_t pos) {
   return s.window && pos >= s.window ? pos - s.window + 1 : 0;
 }
 RC_HD inline int32_t attend_high(const AttendShape& s, int32_t pos) { return pos < 0 ? 0 : pos < s.cap ? pos + 1 : s.cap; }
-RC_HD inline AttendItem attend_item(const AttendShape& s, const AttendRequest& q, int32_t tile) {
-  const int32_t n0 = tile * s.rows, n1 = (q.rows - n0 < s.rows ? q.rows : n0 + s.rows) - 1;
-  const int32_t p0 = q.ctx - q.len + n0 / s.g, p1 = q.ctx - q.len + n1 / s.g;
+// Of rows at positions p0 to p1.
+RC_HD inline AttendItem attend_span(const AttendShape& s, int32_t p0, int32_t p1) {
   AttendItem i;
   i.low_min = attend_low(s, p0), i.low_max = attend_low(s, p1);
   i.high_min = attend_high(s, p0), i.high_max = attend_high(s, p1);
   i.pair0 = i.low_min / kPairTokens;
-  const int32_t end = (int32_t)(((int64_t)i.high_max + kPairTokens - 1) / kPairTokens);
+  const int32_t end = (int32_t)(((uint32_t)i.high_max + kPairTokens - 1) / kPairTokens);
   i.pairs = end > i.pair0 ? end - i.pair0 : 0;
-  const int32_t per = s.unit / kPairTokens;
-  i.units = i.pairs ? (i.pairs + per - 1) / per : 1;
+  // an item that sees nothing has a unit as well: it still has to say so
+  i.free = i.pairs ? s.free : 0;
+  const uint32_t per = s.unit / kPairTokens;
+  i.units = i.pairs ? i.free + (int32_t)((i.pairs + per - 1) / per) : 1;
   return i;
+}
+RC_HD inline AttendItem attend_item(const AttendShape& s, const AttendRequest& q, int32_t tile) {
+  const int32_t n0 = tile * s.rows, n1 = (q.rows - n0 < s.rows ? q.rows : n0 + s.rows) - 1;
+  return attend_span(s, q.ctx - q.len + n0 / s.g, q.ctx - q.len + n1 / s.g);
+}
+// The same where a request has one tile at most.
+RC_HD inline AttendItem attend_only_item(const AttendShape& s, const AttendRequest& q) {
+  const int32_t p0 = q.ctx - q.len;
+  return attend_span(s, p0, p0 + (q.len < s.max_q ? q.len : s.max_q) - 1);
 }
 
 // Units of a request and KV head.
@@ -78,6 +90,13 @@ RC_HD inline int32_t attend_units(const AttendShape& s, const AttendRequest& q) 
   int32_t n = 0;
   for (int32_t t = 0; t < q.tiles; ++t) n += attend_item(s, q, t).units;
   return n;
+}
+
+// The runs of 32 tokens of the part of an item from unit u0 to u1 of its units: [first, last).  A stretch that ends among the free ones
+// leaves the item to the next, which begins it then.
+RC_HD inline int32_t attend_run(const AttendShape& s, const AttendItem& i, int32_t u) {
+  const int64_t n = u > i.free ? (int64_t)(u - i.free) * (s.unit / kPairTokens) : 0;
+  return i.pair0 + (n < i.pairs ? (int32_t)n : i.pairs);
 }
 
 // Units of a workgroup's stretch where there are `total` of them.
@@ -103,21 +122,21 @@ RC_HD inline size_t attend_part_bytes(int32_t rows) { return (size_t)rows * 130 
 constexpr int kWholeTokens = 1024;
 
 struct AttendKernel {
-  int32_t rows, unit, wgs, least;
+  int32_t rows, unit, wgs, least, free;
 };
 // Kernels by the rows of a request and KV head (query tokens times heads of a KV head): tiles of 16 and 32 rows, where every wave
 // of a workgroup has all rows and a quarter of the tokens, and of 128, where every wave has a quarter of the rows.
 inline AttendKernel attend_kernel(int64_t rows) {
-  if (rows <= 16) return {16, 128, 768, 4};
-  if (rows <= 32) return {32, 128, 512, 4};
-  return {128, 64, 512, 8};
+  if (rows <= 16) return {16, 128, 768, 4, 1};
+  if (rows <= 32) return {32, 128, 512, 4, 1};
+  return {128, 64, 512, 8, 1};
 }
 
-// Most units of an item, whatever the lengths: an item of a table's whole length that begins anywhere.
+// Most units of an item, whatever the lengths.
 inline int64_t attend_most_units(const AttendShape& s) {
   const int64_t pairs = ((int64_t)s.cap + kPairTokens - 1) / kPairTokens, per = s.unit / kPairTokens;
   const int64_t n = (pairs + per - 1) / per;
-  return n < 1 ? 1 : n;
+  return n < 1 ? 1 : n + s.free;
 }
 
 // The shape of a call; false where it is beyond what the kernels count in 32 bits.
@@ -128,9 +147,10 @@ inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_
   if (E > (0x7fffffffLL - 64) / T || n_q > 0x7fffffffLL / 2 || R > 0x7fffffffLL / 2 || (max_q > 0 && max_q > 0x7fffff00LL / g)) return false;
   const AttendKernel k = attend_kernel(max_q * g);
   // a window longer than any position is none
-  *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.wgs};
+  *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.free, k.wgs,
+        65536u / (uint32_t)g + 1};
   // a short table: items are not cut, and nothing has to be joined
-  if (s->cap <= kWholeTokens) s->unit = (s->cap + k.unit - 1) / k.unit * k.unit + k.unit, s->least = 1;
+  if (s->cap <= kWholeTokens) s->unit = (s->cap + k.unit - 1) / k.unit * k.unit + k.unit, s->least = 1, s->free = 0;
   // the line is counted in 32 bits: tables long enough for more than 2^30 units have longer ones
   const double items = (double)L * R * H * (((double)max_q * g + k.rows - 1) / k.rows);
   if (items > (1 << 30)) return false;

@@ -101,7 +101,7 @@ struct Walk {
 };
 
 __device__ __forceinline__ void leave_border(const AttendArgs& a, int wg, int last, const Walk& w) {
-  if (a.borders && threadIdx.x == 0) a.borders[wg] = {last, w.at == w.begin, w.l, w.r, w.h, w.t, {0, 0}};
+  if (a.borders && threadIdx.x == 0) a.borders[wg] = {last, w.at == w.begin, w.l, w.h, w.t * a.s.rows, w.q.rows, w.q.first, 0};
 }
 
 // ONE: a request has one row tile at most.
@@ -142,6 +142,7 @@ __device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
   w.begin = w.at = wg * w.share;
   w.end = min(w.at + w.share, line);
   w.l = w.r = w.h = w.t = 0;
+  w.q = {0, 0, 0, 0, 0};
   if (w.at >= line) {
     leave_border(a, wg, -1, w);
     return false;
@@ -332,11 +333,15 @@ template <bool ONE>
 __device__ __forceinline__ int row_token(const AttendArgs& a, int n) {
   return ONE ? (int)((uint32_t)n * a.s.inverse >> 16) : (int)((uint32_t)n / (uint32_t)a.s.g);
 }
-// Row n of the request's, as a row of [L][n_q][n_heads].
+// Row n of a request's rows of a layer and KV head, as a row of [L][n_q][n_heads]; `first` is the request's first query token.
+template <bool ONE>
+__device__ __forceinline__ int64_t row_place(const AttendArgs& a, int l, int h, int first, int n) {
+  const int j = row_token<ONE>(a, n);
+  return ((int64_t)l * a.s.n_q + first + j) * (int64_t)(a.s.H * a.s.g) + h * a.s.g + n - j * a.s.g;
+}
 template <bool ONE>
 __device__ __forceinline__ int64_t row_place(const AttendArgs& a, const Walk& w, int n) {
-  const int j = row_token<ONE>(a, n);
-  return ((int64_t)w.l * a.s.n_q + w.q.first + j) * (int64_t)(a.s.H * a.s.g) + w.h * a.s.g + n - j * a.s.g;
+  return row_place<ONE>(a, w.l, w.h, w.q.first, n);
 }
 __device__ __forceinline__ float row_lse(float ref, float sum) {
   return sum == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
@@ -772,71 +777,62 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
 
 // ---- Items that were cut: a workgroup joins the parts of the item that begins in a stretch and goes on behind it, some rows at a time.
 
-// The sums of row m over the parts first .. last, from the first-th on in steps: x, y for the lane's two dims, and the weights'.
-__device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendBorder& b, int wg, int m, int first, int step, float top, float& x, float& y,
-                                           float& sum) {
-  const int lane = threadIdx.x & 63;
-  x = y = sum = 0.f;
-#pragma unroll 8
-  for (int g = wg + first; g <= b.last; g += step) {
-    const float* p = (const float*)(a.parts + attend_place(g, g > wg || b.begins) * (int64_t)attend_part_bytes(a.s.rows));
-    const float2 s = *(const float2*)(p + a.s.rows * 128 + 2 * m), v = *(const float2*)(p + m * 128 + 2 * lane);
-    const float f = __builtin_amdgcn_exp2f(s.x - top);
-    sum = fmaf(s.y, f, sum);
-    x = fmaf(v.x, f, x);
-    y = fmaf(v.y, f, y);
-  }
+// Eight dims of a row and its softmax.
+struct Joined {
+  f32x4 x, y;
+  float top, sum;
+};
+__device__ __forceinline__ void join(Joined& j, const Joined& k) {
+  const float top = fmaxf(j.top, k.top), f = __builtin_amdgcn_exp2f(j.top - top), g = __builtin_amdgcn_exp2f(k.top - top);
+  j.x = j.x * f + k.x * g;
+  j.y = j.y * f + k.y * g;
+  j.sum = j.sum * f + k.sum * g;
+  j.top = top;
 }
-__device__ __forceinline__ float join_top(const AttendArgs& a, const AttendBorder& b, int wg, int m) {
-  float top = kNothing;
-  for (int g = wg + (threadIdx.x & 63); g <= b.last; g += 64) {
+// Row m over the parts of workgroups g, g + step, .. up to the last: in one pass, so that all loads are on their way at once.
+__device__ __forceinline__ Joined join_parts(const AttendArgs& a, const AttendBorder& b, int wg, int g, int step, int m, int d) {
+  Joined j = {{0, 0, 0, 0}, {0, 0, 0, 0}, kNothing, 0.f};
+#pragma unroll 4
+  for (; g <= b.last; g += step) {
     const float* p = (const float*)(a.parts + attend_place(g, g > wg || b.begins) * (int64_t)attend_part_bytes(a.s.rows));
-    top = fmaxf(top, p[a.s.rows * 128 + 2 * m]);
+    const float2 s = *(const float2*)(p + a.s.rows * 128 + 2 * m);
+    join(j, Joined{*(const f32x4*)(p + m * 128 + d), *(const f32x4*)(p + m * 128 + d + 4), s.x, s.y});
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  return top;
+  return j;
 }
 template <bool BF16>
-__device__ __forceinline__ void join_store(const AttendArgs& a, const Walk& w, int n, float top, float x, float y, float sum) {
-  const int lane = threadIdx.x & 63;
-  const float f = row_scale(sum);
-  const int64_t at = row_place<false>(a, w, n);
-  *(uint32_t*)(a.out + (at * 128 + 2 * lane) * 2) = pack2<BF16>(x * f, y * f);
-  if (lane == 0 && a.lse) a.lse[at] = row_lse(top, sum);
+__device__ __forceinline__ void join_store(const AttendArgs& a, const AttendBorder& b, int m, int d, const Joined& j) {
+  const float f = row_scale(j.sum);
+  const f32x4 x = j.x * f, y = j.y * f;
+  const int64_t at = row_place<false>(a, b.l, b.h, b.first, b.row0 + m);
+  *(u32x4*)(a.out + (at * 128 + d) * 2) = u32x4{pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3])};
+  if (d == 0 && a.lse) a.lse[at] = row_lse(j.top, j.sum);
 }
 
-// FEW rows: a workgroup per row, whose waves share the parts (an item of a long context has up to a hundred); else a wave per row.
+// Sixteen lanes hold a row.  An item of some parts takes sixteen lanes per row; where rows are few, one of many parts (a long context has up to a
+// hundred) takes a workgroup per row, whose sixteen groups of lanes share the parts.
+constexpr int kSomeParts = 8;
+
 template <bool BF16, bool FEW>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
-  __shared__ float2 o[kWaves][64];
-  __shared__ float sums[kWaves];
-  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), wg = blockIdx.x;
+  __shared__ Joined all[16][16];
+  const int i = threadIdx.x & 15, group = threadIdx.x >> 4, d = i * 8, wg = blockIdx.x;
   const AttendBorder b = a.borders[wg];
   if (b.last < 0) return;
-  Walk w;
-  w.l = b.l, w.r = b.r, w.h = b.h, w.t = b.t;
-  w.q = request(a, b.r);
-  const int rows = min(a.s.rows, w.q.rows - b.t * a.s.rows);
-  float x, y, sum;
-  if constexpr (FEW) {
+  const int rows = min(a.s.rows, b.rows - b.row0);
+  if (FEW && b.last - wg >= kSomeParts) {
     const int m = blockIdx.y;
     if (m >= rows) return;
-    const float top = join_top(a, b, wg, m);
-    join_parts(a, b, wg, m, wave, kWaves, top, x, y, sum);
-    o[wave][lane] = float2{x, y};
-    if (lane == 0) sums[wave] = sum;
+    all[group][i] = join_parts(a, b, wg, wg + group, 16, m, d);
     __syncthreads();
-    if (wave) return;
+    if (group) return;
+    Joined j = all[0][i];
 #pragma unroll
-    for (int v = 1; v < kWaves; ++v) x += o[v][lane].x, y += o[v][lane].y, sum += sums[v];
-    join_store<BF16>(a, w, b.t * a.s.rows + m, top, x, y, sum);
+    for (int v = 1; v < 16; ++v) join(j, all[v][i]);
+    join_store<BF16>(a, b, m, d, j);
   } else {
-    for (int m = blockIdx.y * kWaves + wave; m < rows; m += gridDim.y * kWaves) {
-      const float top = join_top(a, b, wg, m);
-      join_parts(a, b, wg, m, 0, 1, top, x, y, sum);
-      join_store<BF16>(a, w, b.t * a.s.rows + m, top, x, y, sum);
-    }
+    const int m = blockIdx.y * 16 + group;
+    if (m < rows) join_store<BF16>(a, b, m, d, join_parts(a, b, wg, wg, 1, m, d));
   }
 }
 

@@ -112,7 +112,8 @@ RC_HD inline int64_t attend_place(int64_t wg, bool begins) { return 2 * wg + (be
 // What a workgroup says of the item that its stretch ends in: where it lies, and up to which workgroup its parts go, if the item begins
 // in this stretch and goes on behind it (else last is -1).
 struct AttendBorder {
-  int32_t last, begins, l, r, h, t, unused[2];
+  int32_t last, begins, l, h;
+  int32_t row0, rows, first, unused;  // the row tile's first row and the request's rows, the request's first query token
 };
 
 // The workspace: a border per workgroup, then the parts, rows x (128 sums, reference, sum of weights) in fp32.

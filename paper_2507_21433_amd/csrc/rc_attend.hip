@@ -668,17 +668,28 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
     };
     const auto attend = [&](int step, int buf) {
       const int pos = (pa + 2 * step) * kPairTokens;
+      // Operands come from LDS four at a time, while the products of the four before them run: left to the compiler, every read is
+      // waited for by itself.
       f32x4 s[RT][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0, 0, 0, 0};
+      u32x4 k[2][4];
+      const auto read_k = [&](int i) {  // tiles 2 (i / 2) and the next, steps 2 (i % 2) and the next
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const u32x4 k = lds.k[buf][j][d][lane];
+        for (int m = 0; m < 4; ++m) k[i & 1][m] = lds.k[buf][(i & 2) + (m & 1)][2 * (i & 1) + (m >> 1)][lane];
+      };
+      read_k(0);
 #pragma unroll
-          for (int t = 0; t < RT; ++t) s[t][j] = mfma<BF16>(k, q[t][d], s[t][j]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        if (i < 3) read_k(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) s[t][(i & 2) + (m & 1)] = mfma<BF16>(k[i & 1][m], q[t][2 * (i & 1) + (m >> 1)], s[t][(i & 2) + (m & 1)]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       const int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
       const bool ends = at_ends(pos);
@@ -706,6 +717,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
           }
         }
       }
+      u32x4 v[2][4];
+      const auto read_v = [&](int i) {  // chunks 4 (i % 2) and the next three of tokens 32 (i / 2) and the next
+#pragma unroll
+        for (int m = 0; m < 4; ++m) v[i & 1][m] = *(const u32x4*)&lds.v[buf][i >> 1][4 * (i & 1) + m][lane][0];
+      };
+      read_v(0);
+      __builtin_amdgcn_sched_barrier(0);
       u32x4 p16[RT][2];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
@@ -723,13 +741,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         }
       }
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int i = 0; i < 4; ++i) {
+        if (i < 3) read_v(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const u32x4 v = *(const u32x4*)&lds.v[buf][j][c][lane][0];
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
-          for (int t = 0; t < RT; ++t) o[t][c] = mfma<BF16>(v, p16[t][j], o[t][c]);
-        }
+          for (int t = 0; t < RT; ++t) o[t][4 * (i & 1) + m] = mfma<BF16>(v[i & 1][m], p16[t][i >> 1], o[t][4 * (i & 1) + m]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     };
 
     Tile x;

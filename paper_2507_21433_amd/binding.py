@@ -442,61 +442,119 @@ def cache_tensor(n_layers, n_blocks, block_tokens, n_kv_heads, device="cuda"):
     return torch.zeros((n_layers, n_blocks, n_kv_heads, block_tokens // 16, RECORD_BYTES), dtype=torch.uint8, device=device)
 
 
-_cdesc = functools.lru_cache(maxsize=64)(CacheDesc)
+# A step's calls on the cache come with the same few layouts again and again, and their kernels take a few microseconds: what a call
+# asks of its tensors' types, shapes and strides is worked out once per layout.  (By these values alone: which tensors they are, and
+# what they hold, is no part of it.)
+def _by_layout(f):
+    return functools.lru_cache(maxsize=256)(f)
 
 
-def _cache_desc(cache, dtype_code):
-    """Descriptor of a cache tensor whose layers are contiguous (the layers themselves may lie apart: some of a larger cache's)."""
-    assert cache.dtype == torch.uint8 and cache.dim() == 5 and cache.shape[4] == RECORD_BYTES, "a cache is uint8 [L][n][H][T/16][2176]"
-    L, n, H, tiles, _ = cache.shape
-    s, block = cache.stride(), H * tiles * RECORD_BYTES
-    assert s[4] == 1 and s[3] == RECORD_BYTES and s[2] == tiles * RECORD_BYTES and (n < 2 or s[1] == block), "a layer of a cache is contiguous"
-    return _cdesc(L, tiles * 16, H, 128, dtype_code, n, s[0] if L > 1 else n * block)
+def _contiguous(shape, strides):
+    step = 1
+    for n, s in zip(reversed(shape), reversed(strides)):
+        if n != 1 and s != step:
+            return 0 in shape
+        step *= n
+    return True
 
 
-def _rows(t):
+_CODES = {torch.float16: RC_F16, torch.bfloat16: RC_BF16}
+
+
+def _code(dtype):
+    if dtype not in _CODES:
+        raise TypeError(f"KV dtype {dtype} (fp16 or bf16 only)")
+    return _CODES[dtype]
+
+
+@_by_layout
+def _cache_desc(shape, s, dtype, code):
+    """Descriptor (by reference) of a cache tensor whose layers are contiguous (the layers may lie apart: some blocks of a larger one's)."""
+    assert dtype == torch.uint8 and len(shape) == 5 and shape[4] == RECORD_BYTES, "a cache is uint8 [L][n][H][T/16][2176]"
+    L, n, H, tiles, _ = shape
+    block = H * tiles * RECORD_BYTES
+    assert s[4] == 1 and (tiles < 2 or s[3] == RECORD_BYTES) and (H < 2 or s[2] == tiles * RECORD_BYTES) and (n < 2 or s[1] == block), \
+        "a layer of a cache is contiguous"
+    return ctypes.byref(CacheDesc(L, tiles * 16, H, 128, code, n, s[0] if L > 1 else n * block))
+
+
+def _row_strides(shape, s):
     """(token stride, layer stride) of a tensor [L][N][heads][128] whose tokens' heads are contiguous."""
-    L, N, heads, D = t.shape
-    s = t.stride()
+    assert len(shape) == 4
+    L, N, heads, D = shape
     assert D == 128 and s[3] == 1 and (heads < 2 or s[2] == 128), "the heads of a token are contiguous"
     token = s[1] if N > 1 else heads * 128
     return token, s[0] if L > 1 else N * token
 
 
+@_by_layout
+def _write_layout(k, ks, kt, v, vs, vt, n, ns, nt, c, cs, ct):
+    assert len(k) == 4 and k == v and kt == vt, "K and V of one type and shape, [L][N][H][128]"
+    L, N, H, _ = k
+    assert len(c) == 5 and c[0] == L and c[2] == H, "K's layers and heads are the cache's"
+    strides = _row_strides(k, ks)
+    assert _row_strides(v, vs) == strides, "K and V of the same strides"
+    assert nt == torch.int32 and n == (N,) and _contiguous(n, ns)
+    return _cache_desc(c, cs, ct, _code(kt)), N, *strides
+
+
 def rc_cache_write(k, v, slots, cache):
     """K and V of new tokens [L][N][H][128] into their slots (block * T + place; int32 [N]) of a 4-bit cache, in place."""
     _dev(k, v, slots, cache)
-    assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype, "K and V of one type and shape, [L][N][H][128]"
-    L, N, H, _ = k.shape
-    assert cache.shape[0] == L and cache.shape[2] == H, "K's layers and heads are the cache's"
-    strides = _rows(k)
-    assert v.stride() == k.stride() or _rows(v) == strides, "K and V of the same strides"
-    assert slots.dtype == torch.int32 and slots.shape == (N,) and slots.is_contiguous()
-    d = _cache_desc(cache, _dtype_code(k))
-    _check(lib().rc_cache_write(ctypes.byref(d), _ptr(k), _ptr(v), N, *strides, _ptr(slots), _ptr(cache), _stream()))
+    d, N, token, layer = _write_layout(k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, slots.shape, slots.stride(), slots.dtype,
+                                       cache.shape, cache.stride(), cache.dtype)
+    code = lib().rc_cache_write(d, k.data_ptr(), v.data_ptr(), N, token, layer, slots.data_ptr(), cache.data_ptr(), _stream())
+    if code:
+        _check(code)
     return cache
+
+
+@_by_layout
+def _read_layout(c, cs, ct, i, is_, it, k, ks, kt, v, vs, vt):
+    assert it == torch.int32 and len(i) == 1 and _contiguous(i, is_)
+    assert len(c) == 5 and k == (c[0], i[0], c[3] * 16, c[2], 128) and v == k, "K and V are [L][n][T][H][128]"
+    L, n, T, H, D = k
+    block = T * H * D
+    assert kt == vt and all(s[4] == 1 and s[3] == D and s[2] == H * D and (n < 2 or s[1] == block) for s in (ks, vs)), "blocks of a layer must be contiguous"
+    layer = ks[0] if L > 1 else n * block
+    assert L < 2 or vs[0] == layer, "K and V of the same strides"
+    return _cache_desc(c, cs, ct, _code(kt)), n, ctypes.byref(KvDesc(L, T, H, D, _code(kt), layer))
 
 
 def rc_cache_read(cache, ids, dtype=None, k=None, v=None):
     """The listed blocks (int32 [n]) of a 4-bit cache, exactly: returns (k, v) [L][n][T][H][128], new ones of `dtype` or the given ones."""
-    _dev(cache, ids, k, v)
-    assert ids.dtype == torch.int32 and ids.dim() == 1 and ids.is_contiguous()
-    L, _, H, tiles, _ = cache.shape
-    shape = (L, ids.numel(), tiles * 16, H, 128)
     if k is None:
-        k = torch.empty(shape, dtype=dtype, device=cache.device)
+        L, _, H, tiles, _ = cache.shape
+        k = torch.empty((L, ids.numel(), tiles * 16, H, 128), dtype=dtype, device=cache.device)
     if v is None:
         v = torch.empty_like(k)
-    assert k.shape == shape
-    _, kd = _kv_pair(k, v, alike=True)
-    d = _cache_desc(cache, kd.dtype)
-    _check(lib().rc_cache_read(ctypes.byref(d), _ptr(cache), _ptr(ids), ids.numel(), ctypes.byref(kd), _ptr(k), _ptr(v), _stream()))
+    _dev(cache, ids, k, v)
+    d, n, kd = _read_layout(cache.shape, cache.stride(), cache.dtype, ids.shape, ids.stride(), ids.dtype, k.shape, k.stride(), k.dtype,
+                            v.shape, v.stride(), v.dtype)
+    code = lib().rc_cache_read(d, cache.data_ptr(), ids.data_ptr(), n, kd, k.data_ptr(), v.data_ptr(), _stream())
+    if code:
+        _check(code)
     return k, v
 
 
 def rc_cache_attend_workspace_size(cache, dtype, R, E, n_heads, max_q=1):
-    d = _cache_desc(cache, RC_F16 if dtype == torch.float16 else RC_BF16)
-    return lib().rc_cache_attend_workspace_size(ctypes.byref(d), R, E, n_heads, max_q)
+    return lib().rc_cache_attend_workspace_size(_cache_desc(cache.shape, cache.stride(), cache.dtype, _code(dtype)), R, E, n_heads, max_q)
+
+
+@_by_layout
+def _attend_layout(q, qs, qt, c, cs, ct, t, ts, tt, x, xs, xt):
+    assert len(q) == 4 and len(t) == 3 and tt == torch.int32 and _contiguous(t, ts), "tables are int32 [L][R][E]"
+    L, N, heads, _ = q
+    _, R, E = t
+    assert len(c) == 5 and c[0] == L and t[0] == L, "the queries' layers are the cache's and the tables'"
+    assert xt == torch.int32 and x == (R,) and _contiguous(x, xs)
+    return _cache_desc(c, cs, ct, _code(qt)), L, N, heads, R, E, *_row_strides(q, qs)
+
+
+@_by_layout
+def _attend_out(q, qt, o, os_, ot, e, es, et):
+    assert o == q and ot == qt and _contiguous(o, os_), "out is [L][N][heads][128] of the queries' type"
+    assert e is None or (e == q[:3] and et == torch.float32 and _contiguous(e, es)), "lse is float32 [L][N][heads]"
 
 
 def rc_cache_attend(q, cache, tables, ctx_len, q_start=None, max_q=1, scale=None, window=0, want_lse=True, workspace=None, out=None,
@@ -505,25 +563,25 @@ def rc_cache_attend(q, cache, tables, ctx_len, q_start=None, max_q=1, scale=None
 
     ctx_len int32 [R]: cached tokens, this step's among them; q_start int32 [R+1]: a request's query tokens (None: one each);
     max_q: most query tokens of a request.  Returns dict(out [L][N][heads][128], lse float32 [L][N][heads] or None)."""
+    shape, dtype = q.shape, q.dtype
+    d, L, N, heads, R, E, token, layer = _attend_layout(shape, q.stride(), dtype, cache.shape, cache.stride(), cache.dtype, tables.shape,
+                                                        tables.stride(), tables.dtype, ctx_len.shape, ctx_len.stride(), ctx_len.dtype)
     _dev(q, cache, tables, ctx_len, q_start, workspace, out, lse)
-    assert q.dim() == 4 and tables.dim() == 3 and tables.dtype == torch.int32 and tables.is_contiguous()
-    L, N, heads, _ = q.shape
-    _, R, E = tables.shape
-    assert cache.shape[0] == L and tables.shape[0] == L, "the queries' layers are the cache's and the tables'"
-    assert ctx_len.dtype == torch.int32 and ctx_len.shape == (R,) and ctx_len.is_contiguous()
     if q_start is not None:
         assert q_start.dtype == torch.int32 and q_start.shape == (R + 1,) and q_start.is_contiguous()
-    d = _cache_desc(cache, _dtype_code(q))
     if workspace is None:
-        workspace = torch.empty(max(16, lib().rc_cache_attend_workspace_size(ctypes.byref(d), R, E, heads, max_q)), dtype=torch.uint8,
-                                device=q.device)
+        workspace = torch.empty(max(16, lib().rc_cache_attend_workspace_size(d, R, E, heads, max_q)), dtype=torch.uint8, device=q.device)
     if out is None:
-        out = torch.empty((L, N, heads, 128), dtype=q.dtype, device=q.device)
+        out = torch.empty((L, N, heads, 128), dtype=dtype, device=q.device)
     if lse is None and want_lse:
         lse = torch.empty((L, N, heads), dtype=torch.float32, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
-    assert lse is None or (lse.shape == (L, N, heads) and lse.dtype == torch.float32 and lse.is_contiguous())
-    _check(lib().rc_cache_attend(ctypes.byref(d), _ptr(cache), _ptr(tables), R, E, _ptr(ctx_len), _ptr(q_start), _ptr(q), N, heads,
-                                 *_rows(q), max_q, 128 ** -0.5 if scale is None else float(scale), int(window), _ptr(out), _ptr(lse),
-                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+    if lse is None:
+        _attend_out(shape, dtype, out.shape, out.stride(), out.dtype, None, None, None)
+    else:
+        _attend_out(shape, dtype, out.shape, out.stride(), out.dtype, lse.shape, lse.stride(), lse.dtype)
+    code = lib().rc_cache_attend(d, cache.data_ptr(), tables.data_ptr(), R, E, ctx_len.data_ptr(), None if q_start is None else q_start.data_ptr(),
+                                 q.data_ptr(), N, heads, token, layer, max_q, 128 ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                                 None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream())
+    if code:
+        _check(code)
     return dict(out=out, lse=lse)

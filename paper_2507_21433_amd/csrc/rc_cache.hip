@@ -15,8 +15,8 @@ struct WriteArgs {
   const int32_t* slots;
   char* cache;
   int64_t token_stride_b, kv_layer_stride_b, cache_layer_stride;
-  int64_t waves;  // groups of 16 tokens x heads, of a layer
   int64_t n_slots;
+  uint32_t waves;  // groups of 16 tokens x heads, of a layer
   int32_t N, H, tiles;
 };
 
@@ -78,10 +78,10 @@ __device__ __forceinline__ uint32_t quantise(u32x4 x, uint32_t& byte) {
 template <bool BF16>
 __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(WriteArgs a) {
   const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
-  const int64_t w = (int64_t)blockIdx.x * (kCacheThreads / 64) + (threadIdx.x >> 6);
+  const uint32_t w = blockIdx.x * (kCacheThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (w >= a.waves) return;
-  const int h = (int)(w % a.H);
-  const int64_t n0 = w / a.H * 16 + 4 * q, l = blockIdx.y;
+  const int h = (int)(w % (uint32_t)a.H);
+  const int64_t n0 = (int64_t)(w / (uint32_t)a.H) * 16 + 4 * q, l = blockIdx.y;
   const int64_t off = l * a.kv_layer_stride_b + (int64_t)h * 256 + i * 16;
   u32x4 kx[4], vx[4];
   int slot[4];
@@ -104,8 +104,8 @@ __global__ __launch_bounds__(kCacheThreads) void cache_write_kernel(WriteArgs a)
     const uint32_t kw = quantise<BF16>(kx[r], kb), vw = quantise<BF16>(vx[r], vb);
     if (slot[r] >= 0) {
       const int tile = slot[r] >> 4, t = slot[r] & 15;
-      const int64_t block = tile / a.tiles;
-      char* rec = layer + ((block * a.H + h) * a.tiles + tile % a.tiles) * kRecordBytes;
+      const int64_t block = tile >> (a.tiles - 1);  // of one tile or two
+      char* rec = layer + ((block * a.H + h) * a.tiles + (tile & (a.tiles - 1))) * kRecordBytes;
       *(uint32_t*)(rec + ((i >> 2) * 16 + t) * 16 + (i & 3) * 4) = kw;
       *(uint32_t*)(rec + kRecordV + ((t >> 2) * 16 + i) * 16 + (t & 3) * 4) = vw;
       if ((i & 3) == 0) {
@@ -121,7 +121,7 @@ struct ReadArgs {
   const int32_t* ids;
   char *k, *v;
   int64_t cache_layer_stride, kv_layer_stride_b, n_blocks;
-  int64_t waves;  // records of a layer
+  uint32_t waves;  // records of a layer
   int32_t H, tiles;
 };
 
@@ -130,13 +130,12 @@ struct ReadArgs {
 template <bool BF16>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(ReadArgs a) {
   const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
-  const int64_t w = (int64_t)blockIdx.x * (kCacheThreads / 64) + (threadIdx.x >> 6);
+  const uint32_t w = blockIdx.x * (kCacheThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (w >= a.waves) return;
-  const int h = (int)(w % a.H);
-  const int64_t row = w / a.H;  // tile of the output
-  const int64_t n = row / a.tiles, l = blockIdx.y;
-  const int tile = (int)(row % a.tiles);
-  const int id = a.ids[n];
+  const int h = (int)(w % (uint32_t)a.H);
+  const int64_t row = w / (uint32_t)a.H, l = blockIdx.y;  // row: tile of the output
+  const int tile = (int)row & (a.tiles - 1);               // of one tile or two
+  const int id = a.ids[row >> (a.tiles - 1)];
   uint32_t kw[4] = {0, 0, 0, 0}, kb = 0, vb = 0;
   u32x4 vw = {0, 0, 0, 0};
   if (id >= 0 && id < a.n_blocks) {
@@ -182,7 +181,7 @@ extern "C" rc_status rc_cache_write(const rc_cache_desc* cdesc, const void* k, c
     return fail(RC_ERR_INVALID_ARG, "%s: token_stride smaller than H*Dh, or a stride that breaks 16-byte alignment", who);
   if (cdesc->n_layers > 1 && kv_layer_stride < H * 128) return fail(RC_ERR_INVALID_ARG, "%s: kv_layer_stride smaller than a token", who);
   WriteArgs a = {(const char*)k, (const char*)v, slots, (char*)cache, token_stride * 2, kv_layer_stride * 2, cdesc->layer_stride,
-                 (n_tokens + 15) / 16 * H, cdesc->n_blocks * cdesc->block_tokens, (int32_t)n_tokens, H, cdesc->block_tokens / 16};
+                 cdesc->n_blocks * cdesc->block_tokens, (uint32_t)((n_tokens + 15) / 16 * H), (int32_t)n_tokens, H, cdesc->block_tokens / 16};
   const dim3 grid((unsigned)((a.waves + 3) / 4), (unsigned)cdesc->n_layers);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (cdesc->dtype == RC_BF16)
@@ -208,7 +207,7 @@ extern "C" rc_status rc_cache_read(const rc_cache_desc* cdesc, const void* cache
   if (!cache || !ids || !k || !v) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
   if (!aligned16(cache) || !aligned16(k) || !aligned16(v)) return fail(RC_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
   ReadArgs a = {(const char*)cache, ids, (char*)k, (char*)v, cdesc->layer_stride, kvdesc->layer_stride * 2, cdesc->n_blocks,
-                n * tiles * H, H, tiles};
+                (uint32_t)(n * tiles * H), H, tiles};
   const dim3 grid((unsigned)((a.waves + 3) / 4), (unsigned)cdesc->n_layers);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (cdesc->dtype == RC_BF16)

@@ -228,10 +228,22 @@ struct Tile {
   uint32_t ke, ve;
 };
 
-__device__ __forceinline__ void load_tile(Tile& x, const char* rec, int lane) {
-  x.k = *(const u32x4*)(rec + lane * 16);
-  x.v = *(const u32x4*)(rec + kRecordV + lane * 16);
+// STREAM: codes that no other workgroup reads are not kept in the caches behind this one, where there are too many of them anyway.
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load_codes(const char* p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load((const u32x4*)p);
+  else
+    return *(const u32x4*)p;
+}
+template <bool STREAM>
+__device__ __forceinline__ void load_k(Tile& x, const char* rec, int lane) {
+  x.k = load_codes<STREAM>(rec + lane * 16);
   x.ke = *(const uint8_t*)(rec + kRecordKExp + lane);
+}
+template <bool STREAM>
+__device__ __forceinline__ void load_v(Tile& x, const char* rec, int lane) {
+  x.v = load_codes<STREAM>(rec + kRecordV + lane * 16);
   x.ve = *(const uint32_t*)(rec + kRecordVExp + ((lane >> 4) * 4 + ((lane & 15) >> 2)) * 4);
 }
 
@@ -377,8 +389,14 @@ struct RowsLds {
   float o[kWaves][16][132];
 };
 
-template <bool BF16, int RT>
+// What bounds it is memory: 64 requests of up to 12.4k tokens 580 MB in 107 us (5.4 TB/s; a plain read of as much 113).  Three waves a SIMD of one
+// row tile: with four (128 registers) 153 us instead of 118, with touches of the lines of the pairs to come 147: 32 KB of lines is all that a compute
+// unit's cache holds on their way.  Each wave's K is loaded again where it is used up, and so is V; held twice, whole pairs ahead, 121.
+template <bool BF16, int RT, bool STREAM>
 __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(AttendArgs a) {
+  // Probabilities as sums of two 16-bit numbers: with one row tile the matrix cores have the time (1 to 5 % of a call), and the only rounding
+  // that counts is that of the output; with two tiles it is 10 %, and they are rounded once, which in the output is as much as its own rounding.
+  constexpr bool kTwo = RT == 1;
   __shared__ RowsLds<RT> lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   // neighbouring stretches to one XCD: row tiles of a request and head read the same cache
@@ -402,16 +420,6 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 
     // the wave's pairs of tiles: every fourth from pa + wave on
     const int mine = (part.pb - part.pa - wave + kWaves - 1) / kWaves;
-    int ids = -1;
-    const auto load = [&](Tile (&x)[2], int (&there)[2], int n) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        bool is;
-        load_tile(x[j], record(a, head, ids, 2 * (n & 31) + j, j, is), lane);
-        there[j] = is;
-      }
-    };
-
     u32x4 q[RT][4];
     f32x4 o[RT][8];
     float ref[RT], sum[RT];
@@ -427,36 +435,45 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       ref[t] = kNothing, sum[t] = 0.f;
     }
 
-    Tile x[2], y[2];
-    int there[2], there_y[2] = {0, 0};
-    // The loads of the next pair are in flight while one is worked on.  They are never left out (behind the last pair that one is
-    // loaded again): where a branch goes round them, the wait for this pair's loads becomes a wait for all.  The first round only loads.
-#pragma unroll 1
-    for (int n = -1; n < mine; ++n) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) x[j] = y[j], there[j] = there_y[j];
-      const int next = min(n + 1, mine - 1);
-      if ((n & 31) == 31 && next > n) {
-        const int pair = part.pa + wave + kWaves * (next + (lane >> 1));
+    Tile x[2];
+    const char* rec[2];
+    bool there[2], there_next[2] = {false, false};
+    int ids = -1;
+    const auto find_records = [&](int n) {
+      if ((n & 31) == 0) {
+        const int pair = part.pa + wave + kWaves * (n + (lane >> 1));
         ids = load_id(a, table, 2 * pair + (lane & 1), pair < part.pb);
       }
-      if (mine > 0) load(y, there_y, next);
-      if (n < 0) continue;
-
+#pragma unroll
+      for (int j = 0; j < 2; ++j) rec[j] = record(a, head, ids, 2 * (n & 31) + j, j, there_next[j]);
+    };
+    if (mine) {
+      find_records(0);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_k<STREAM>(x[j], rec[j], lane), load_v<STREAM>(x[j], rec[j], lane);
+    }
+    // The next pair's K is on its way from where this one's is used up, and V likewise.  The loads are never left out (behind the
+    // last pair that one is loaded again): where a branch goes round them, a wait for some of the loads becomes a wait for all.
+#pragma unroll 1
+    for (int n = 0; n < mine; ++n) {
       const int pair = part.pa + wave + kWaves * n, pos = pair * kPairTokens;
+      there[0] = there_next[0], there[1] = there_next[1];
       f32x4 s[RT][2];
+      const float power[2] = {power_of(x[0].ke), power_of(x[1].ke)};
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float power = power_of(x[j].ke);
+      for (int d = 0; d < 4; ++d) {
+        u32x4 k[2];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0, 0, 0, 0};
+        for (int j = 0; j < 2; ++j) k[j] = unpack8<BF16>(x[j].k[d], power[j]);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const u32x4 k = unpack8<BF16>(x[j].k[d], power);
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int t = 0; t < RT; ++t) s[t][j] = mfma<BF16>(k, q[t][d], s[t][j]);
-        }
+          for (int j = 0; j < 2; ++j) s[t][j] = mfma<BF16>(k[j], q[t][d], d ? s[t][j] : f32x4{0, 0, 0, 0});
       }
+      if (n + 1 < mine) find_records(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_k<STREAM>(x[j], rec[j], lane);
       // every row sees all 32 tokens, but at the ends of what the rows see and where the table has a hole
       if (pos < w.item.low_max || pos + kPairTokens > w.item.high_min || !there[0] || !there[1]) {
         uint32_t flags = 0, seen[RT];
@@ -495,13 +512,11 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], a.c, -ref[t]));
         sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        // a probability as the sum of two 16-bit numbers: the matrix cores have the time for the second product here, and the
-        // only rounding that counts is then that of the output
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t two = cut2<BF16>(p[2 * j], p[2 * j + 1]);
+          const uint32_t two = kTwo ? cut2<BF16>(p[2 * j], p[2 * j + 1]) : pack2<BF16>(p[2 * j], p[2 * j + 1]);
           hi[t][j] = two;
-          lo[t][j] = cut2<BF16>(p[2 * j] - low16<BF16>(two), p[2 * j + 1] - high16<BF16>(two));
+          if (kTwo) lo[t][j] = cut2<BF16>(p[2 * j] - low16<BF16>(two), p[2 * j + 1] - high16<BF16>(two));
         }
       }
       float p0[4], p1[4];
@@ -517,14 +532,20 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
         for (int t = 0; t < RT; ++t) {
           o[t][2 * B] = mfma<BF16>(even, hi[t], o[t][2 * B]);
           o[t][2 * B + 1] = mfma<BF16>(odd, hi[t], o[t][2 * B + 1]);
-          o[t][2 * B] = mfma<BF16>(even, lo[t], o[t][2 * B]);
-          o[t][2 * B + 1] = mfma<BF16>(odd, lo[t], o[t][2 * B + 1]);
+          if (kTwo) {
+            o[t][2 * B] = mfma<BF16>(even, lo[t], o[t][2 * B]);
+            o[t][2 * B + 1] = mfma<BF16>(odd, lo[t], o[t][2 * B + 1]);
+          }
         }
+
       };
       chunks(std::integral_constant<int, 0>{});
       chunks(std::integral_constant<int, 1>{});
       chunks(std::integral_constant<int, 2>{});
       chunks(std::integral_constant<int, 3>{});
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], rec[j], lane);
     }
 
     // the four waves' sums, under the largest of their references
@@ -638,7 +659,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         const int pair = pa + 2 * (step + lane) + (wave >> 1);
         ids = load_id(a, table, 2 * pair + (wave & 1), pair < pb);
       }
-      load_tile(x, record(a, head, ids, step & 63, wave & 1, there), lane);
+      const char* rec = record(a, head, ids, step & 63, wave & 1, there);
+      load_k<false>(x, rec, lane);
+      load_v<false>(x, rec, lane);
     };
     const auto unpack = [&](const Tile& x, bool there, int step, int buf) {
       const int pos = (pa + 2 * step) * kPairTokens;
@@ -684,12 +707,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i < 3) read_k(i + 1);
-        __builtin_amdgcn_sched_barrier(0);
+
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
           for (int t = 0; t < RT; ++t) s[t][(i & 2) + (m & 1)] = mfma<BF16>(k[i & 1][m], q[t][2 * (i & 1) + (m >> 1)], s[t][(i & 2) + (m & 1)]);
-        __builtin_amdgcn_sched_barrier(0);
+
       }
       const int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
       const bool ends = at_ends(pos);
@@ -743,12 +766,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i < 3) read_v(i + 1);
-        __builtin_amdgcn_sched_barrier(0);
+
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
           for (int t = 0; t < RT; ++t) o[t][4 * (i & 1) + m] = mfma<BF16>(v[i & 1][m], p16[t][i >> 1], o[t][4 * (i & 1) + m]);
-        __builtin_amdgcn_sched_barrier(0);
+
       }
     };
 
@@ -871,10 +894,11 @@ rc_status attend_check(const rc_cache_desc* d, int64_t R, int64_t E, int32_t n_h
 template <bool BF16>
 void attend_launch(const AttendArgs& a, hipStream_t st) {
   const dim3 grid(a.s.wgs);
+  const bool stream = attend_streams(a.s);
   if (a.s.rows == 16)
-    attend_rows_kernel<BF16, 1><<<grid, kThreads, 0, st>>>(a);
+    stream ? attend_rows_kernel<BF16, 1, true><<<grid, kThreads, 0, st>>>(a) : attend_rows_kernel<BF16, 1, false><<<grid, kThreads, 0, st>>>(a);
   else if (a.s.rows == 32)
-    attend_rows_kernel<BF16, 2><<<grid, kThreads, 0, st>>>(a);
+    stream ? attend_rows_kernel<BF16, 2, true><<<grid, kThreads, 0, st>>>(a) : attend_rows_kernel<BF16, 2, false><<<grid, kThreads, 0, st>>>(a);
   else
     attend_many_kernel<BF16><<<grid, kThreads, 0, st>>>(a);
   if (!a.borders) return;

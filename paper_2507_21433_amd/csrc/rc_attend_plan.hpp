@@ -164,6 +164,12 @@ inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_
   if (most < s->wgs) s->wgs = ((int32_t)most + 8) / 8 * 8;
   return true;
 }
+// Whether a call's tables can hold more than the last-level cache (256 MB on an MI355X) keeps from one pass over them to the next: its codes
+// are then loaded without being kept.  us, kept -> not: 580 MB 118 -> 113, 416 MB 87.5 -> 84.7, 285 MB 62.7 -> 63.1, 160 MB 39.6 -> 43.3, 94 MB 35.3 -> 37.0.
+inline bool attend_streams(const AttendShape& s) {
+  const double seen = s.window && (double)s.window + s.max_q < s.cap ? (double)s.window + s.max_q : s.cap;
+  return (double)s.L * s.R * s.H * seen * 136 > 384e6;
+}
 // Parts of a call, at most, and its workspace.
 inline int64_t attend_most_parts(const AttendShape& s) { return attend_most_units(s) > 1 ? 2 * (int64_t)s.wgs : 0; }
 inline size_t attend_workspace(const AttendShape& s) {

@@ -161,7 +161,7 @@ class Problem:
             rc.rc_cache_write(self.k.to(DEV), self.v.to(DEV), slots.to(DEV), self.cache)
         self.q = randn((L, N, H * g, 128), gn, dtype).to(DEV)
         self.scale, self.window, self.max_q = 128 ** -0.5, 0, max(self.new)
-        self.many = self.max_q * g > 32
+        self.many = self.max_q * g > 16      # probabilities rounded once
 
     def run(self, **kw):
         i = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
@@ -233,6 +233,14 @@ def test_table_shorter_than_the_context():
     for q, g in ((1, 5), (30, 4)):
         p = Problem([(400, q), (100, q)], 2, g, 16, BF, E=13)
         p.check(p.run())
+
+
+@pytest.mark.parametrize("m,g,T,dtype", [(1, 4, 16, HALF), (1, 1, 32, BF), (4, 7, 32, HALF), (6, 5, 16, BF), (40, 2, 16, BF)])
+def test_tables_with_room_for_more_than_the_caches_hold(m, g, T, dtype):
+    """Rows of a table that could list 800 MB of cache and list some KB: the calls that load codes without keeping them."""
+    E = 1_500_000 // T
+    p = Problem([(700, m), (3000, m), (33, m), (0, m)], 2, g, T, dtype, E=E)
+    p.check(p.run())
 
 
 @pytest.mark.parametrize("dtype", [HALF, BF])

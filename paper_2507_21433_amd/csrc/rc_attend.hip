@@ -600,7 +600,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
   }
 }
 
-// ---- Many rows: every wave has 32 of an item's 128 rows, and the workgroup turns 64 tokens at a time into operands in LDS.
+// ---- Many rows: every wave has 32 of an item's 128 rows (16 of 64 with one row tile), and the workgroup turns 64 tokens at a time into operands in LDS.
 
 struct ManyLds {
   u32x4 k[2][4][4][64];  // [buffer][16 tokens][step of the dims][lane]
@@ -609,9 +609,9 @@ struct ManyLds {
   int32_t there[2][4];
 };
 
-template <bool BF16>
+template <bool BF16, int RT>
 __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) {
-  constexpr int RT = 2, kStep = 64, kRows = 128;
+  constexpr int kStep = 64, kRows = kWaves * 16 * RT;
   __shared__ ManyLds lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
@@ -899,8 +899,10 @@ void attend_launch(const AttendArgs& a, hipStream_t st) {
     stream ? attend_rows_kernel<BF16, 1, true><<<grid, kThreads, 0, st>>>(a) : attend_rows_kernel<BF16, 1, false><<<grid, kThreads, 0, st>>>(a);
   else if (a.s.rows == 32)
     stream ? attend_rows_kernel<BF16, 2, true><<<grid, kThreads, 0, st>>>(a) : attend_rows_kernel<BF16, 2, false><<<grid, kThreads, 0, st>>>(a);
+  else if (a.s.rows == 64)
+    attend_many_kernel<BF16, 1><<<grid, kThreads, 0, st>>>(a);
   else
-    attend_many_kernel<BF16><<<grid, kThreads, 0, st>>>(a);
+    attend_many_kernel<BF16, 2><<<grid, kThreads, 0, st>>>(a);
   if (!a.borders) return;
   const int64_t rows = (int64_t)a.s.max_q * a.s.g;
   if (a.s.rows <= 32)

@@ -126,10 +126,11 @@ struct AttendKernel {
   int32_t rows, unit, wgs, least, free;
 };
 // Kernels by the rows of a request and KV head (query tokens times heads of a KV head): tiles of 16 and 32 rows, where every wave
-// of a workgroup has all rows and a quarter of the tokens, and of 128, where every wave has a quarter of the rows.
+// of a workgroup has all rows and a quarter of the tokens, and of 64 and 128, where every wave has a quarter of the rows.
 inline AttendKernel attend_kernel(int64_t rows) {
   if (rows <= 16) return {16, 128, 768, 4, 1};
   if (rows <= 32) return {32, 128, 512, 4, 1};
+  if (rows <= 64) return {64, 64, 512, 8, 1};
   return {128, 64, 512, 8, 1};
 }
 

@@ -663,20 +663,21 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
       load_k<false>(x, rec, lane);
       load_v<false>(x, rec, lane);
     };
-    const auto unpack = [&](const Tile& x, bool there, int step, int buf) {
+    const auto check = [&](Tile& x, bool there, int step, int buf) {
       const int pos = (pa + 2 * step) * kPairTokens;
-      uint32_t ve = x.ve;
       if (at_ends(pos) || !there) {
-        ve = seen_only(ve, pos + 16 * wave + 4 * quarter, there, w.item);
-        if ((col & 3) == 0) lds.ve[buf][wave][quarter * 4 + (col >> 2)] = ve;
-        ve = without_nans(ve, nan_bytes(ve));
+        x.ve = seen_only(x.ve, pos + 16 * wave + 4 * quarter, there, w.item);
+        if ((col & 3) == 0) lds.ve[buf][wave][quarter * 4 + (col >> 2)] = x.ve;
+        x.ve = without_nans(x.ve, nan_bytes(x.ve));
       }
       if (lane == 0) lds.there[buf][wave] = there;
+    };
+    const auto unpack = [&](const Tile& x, int buf) {
       const float power = power_of(x.ke);
 #pragma unroll
       for (int d = 0; d < 4; ++d) lds.k[buf][wave][d][lane] = unpack8<BF16>(x.k[d], power);
       float p[4];
-      powers(ve, p);
+      powers(x.ve, p);
       const auto chunks = [&](auto b) {
         constexpr int B = decltype(b)::value;
         uint32_t e[2], d[2];
@@ -689,7 +690,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
       chunks(std::integral_constant<int, 2>{});
       chunks(std::integral_constant<int, 3>{});
     };
-    const auto attend = [&](int step, int buf) {
+    const auto attend = [&](Tile& x, bool there_next, int step, int buf) {
       const int pos = (pa + 2 * step) * kPairTokens;
       // Operands come from LDS four at a time, while the products of the four before them run: left to the compiler, every read is
       // waited for by itself.
@@ -707,12 +708,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (i < 3) read_k(i + 1);
-
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
           for (int t = 0; t < RT; ++t) s[t][(i & 2) + (m & 1)] = mfma<BF16>(k[i & 1][m], q[t][2 * (i & 1) + (m >> 1)], s[t][(i & 2) + (m & 1)]);
-
+        __builtin_amdgcn_sched_barrier(0);
       }
       const int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
       const bool ends = at_ends(pos);
@@ -740,53 +741,78 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
           }
         }
       }
-      u32x4 v[2][4];
-      const auto read_v = [&](int i) {  // chunks 4 (i % 2) and the next three of tokens 32 (i / 2) and the next
-#pragma unroll
-        for (int m = 0; m < 4; ++m) v[i & 1][m] = *(const u32x4*)&lds.v[buf][i >> 1][4 * (i & 1) + m][lane][0];
-      };
-      read_v(0);
-      __builtin_amdgcn_sched_barrier(0);
-      u32x4 p16[RT][2];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         float top = s[t][0][0];
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
         rescale<8>(o[t], ref[t], sum[t], top, a.c);
-        float p[16];
+      }
+      check(x, there_next, step + 1, buf ^ 1);
+      u32x4 v[8], p16[RT][2];
+      const auto read_v = [&](int i) {  // the chunks of tokens 32 i and the next
 #pragma unroll
-        for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], a.c, -ref[t]));
+        for (int c = 0; c < 8; ++c) v[c] = *(const u32x4*)&lds.v[buf][i][c][lane][0];
+      };
+      const auto weigh = [&](int i) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          sum[t] += p[2 * j] + p[2 * j + 1];
-          p16[t][j >> 2][j & 3] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
+        for (int t = 0; t < RT; ++t) {
+          float p[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + (j >> 2)][j & 3], a.c, -ref[t]));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p16[t][i][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
+          sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         }
+      };
+      const auto add = [&](int i) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) o[t][c] = mfma<BF16>(v[c], p16[t][i], o[t][c]);
+      };
+      // The products of the first 32 tokens run beside the exponentials of the other 32, and theirs beside the next step's unpacking.
+      read_v(0);
+      __builtin_amdgcn_sched_barrier(0);
+      weigh(0);
+      __builtin_amdgcn_sched_barrier(0);
+      add(0);
+      weigh(1);
+#pragma unroll
+      for (int i = 0; i < 8 * RT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      read_v(1);
+      add(1);
+      unpack(x, buf ^ 1);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i < 3) read_v(i + 1);
-
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-          for (int t = 0; t < RT; ++t) o[t][4 * (i & 1) + m] = mfma<BF16>(v[i & 1][m], p16[t][i >> 1], o[t][4 * (i & 1) + m]);
-
+      for (int i = 0; i < 8 * RT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x2, 4, 1);
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 1);
       }
+      __builtin_amdgcn_sched_barrier(0);
     };
 
     Tile x;
     bool there;
     if (steps > 0) {
       load(x, there, 0);
-      unpack(x, there, 0, 0);
+      check(x, there, 0, 0);
+      unpack(x, 0);
     }
     __syncthreads();
+    // behind the last step a tile of no block is loaded and unpacked into the buffer that is free
     for (int step = 0; step < steps; ++step) {
-      const bool more = step + 1 < steps;
-      if (more) load(x, there, step + 1);
-      if (busy) attend(step, step & 1);
-      if (more) unpack(x, there, step + 1, (step + 1) & 1);
+      load(x, there, step + 1);
+      if (busy) {
+        attend(x, there, step, step & 1);
+      } else {
+        check(x, there, step + 1, ~step & 1);
+        unpack(x, ~step & 1);
+      }
       __syncthreads();
     }
 

@@ -120,17 +120,24 @@ struct AttendBorder {
 RC_HD inline size_t attend_header_bytes(int32_t wgs) { return (size_t)wgs * sizeof(AttendBorder); }
 RC_HD inline size_t attend_part_bytes(int32_t rows) { return (size_t)rows * 130 * 4; }
 
+// Tables of up to so many tokens: items are not cut, and no second launch joins them.  us, not cut -> cut: 64 requests of up to 1000 tokens
+// 19.2 -> 21.3, one of 900 11.6 -> 13.9; of 2000: 8 requests 18.7 -> 15.8, 40 requests 26.9 -> 23.6.
 constexpr int kWholeTokens = 1024;
 
 struct AttendKernel {
   int32_t rows, unit, wgs, least, free;
 };
 // Kernels by the rows of a request and KV head (query tokens times heads of a KV head): tiles of 16 and 32 rows, where every wave
-// of a workgroup has all rows and a quarter of the tokens, and of 64 and 128, where every wave has a quarter of the rows.
-inline AttendKernel attend_kernel(int64_t rows) {
-  if (rows <= 16) return {16, 128, 768, 4, 1};
+// of a workgroup has all rows and a quarter of the tokens, and of 64 and 128, where every wave has a quarter of the rows.  64 also for
+// more rows where tiles of 128 would be few and their work small (`pairs` (layers, requests and heads) times `steps` of 64 tokens): more
+// workgroups with less to do each.  us, tiles of 128 -> 64: 32 tiles of 900 tokens 31 -> 26, 16 of 8192 37 -> 31; 160 of 512 30 -> 34, 64 of 60000 268 -> 352.
+// A stretch has `least` units at least (2, 4, 8 and 16 tried: one request of 4096 tokens 14.1, 13.4, 15.2 and 19.6), an item costs `free` units more
+// than its tokens (0, 1 and 2: 40 requests of 2000 tokens 23.6, 23.6 and 22.3; drafts of 20 requests 33.7, 31.4 and 31.8).
+inline AttendKernel attend_kernel(int64_t rows, double pairs, int64_t steps) {
+  if (rows <= 16) return {16, 128, 768, 4, 2};
   if (rows <= 32) return {32, 128, 512, 4, 1};
-  if (rows <= 64) return {64, 64, 512, 8, 1};
+  const double tiles = pairs * (double)((rows + 127) / 128);
+  if (rows <= 64 || (tiles <= 128 && tiles * (double)steps <= 16384)) return {64, 64, 512, 8, 1};
   return {128, 64, 512, 8, 1};
 }
 
@@ -147,7 +154,7 @@ inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_
   const int32_t g = n_heads / H;
   if (max_q > n_q) max_q = n_q;
   if (E > (0x7fffffffLL - 64) / T || n_q > 0x7fffffffLL / 2 || R > 0x7fffffffLL / 2 || (max_q > 0 && max_q > 0x7fffff00LL / g)) return false;
-  const AttendKernel k = attend_kernel(max_q * g);
+  const AttendKernel k = attend_kernel(max_q * g, (double)L * R * H, E * T / 64);
   // a window longer than any position is none
   *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.free, k.wgs,
         65536u / (uint32_t)g + 1};

@@ -183,6 +183,8 @@ class Problem:
             assert (off <= b).all(), name
 
 
+WIDE = 40000        # entries of a table: items may be cut however short they are, and many rows go in tiles of 128 instead of 64
+
 SHAPES = {
     "one token": [(1, 1)],
     "two": [(2, 1), (1, 1)],
@@ -200,27 +202,28 @@ SHAPES = {
 
 @pytest.mark.parametrize("H,g,T,dtype", [(2, 5, 16, HALF), (1, 1, 32, BF), (3, 4, 16, BF), (2, 8, 32, HALF), (1, 16, 16, BF), (2, 7, 32, HALF)])
 @pytest.mark.parametrize("shape", sorted(SHAPES))
-def test_attend(shape, H, g, T, dtype):
-    say(shape, H, g, T, dtype)
-    p = Problem(SHAPES[shape], H, g, T, dtype, strong=g == 5)
+@pytest.mark.parametrize("E", [None, WIDE])
+def test_attend(shape, H, g, T, dtype, E):
+    say(shape, H, g, T, dtype, E)
+    p = Problem(SHAPES[shape], H, g, T, dtype, E=E, strong=g == 5)
     p.check(p.run())
 
 
 @pytest.mark.parametrize("window", [1, 16, 33, 200, 100000])
 @pytest.mark.parametrize("shape", ["draft", "cut", "chunk", "more queries than tokens"])
-@pytest.mark.parametrize("T,dtype", [(16, BF), (32, HALF)])
-def test_window(shape, window, T, dtype):
-    say(shape, window, T, dtype)
-    p = Problem(SHAPES[shape], 2, 4, T, dtype)
+@pytest.mark.parametrize("T,dtype,E", [(16, BF, None), (32, HALF, WIDE)])
+def test_window(shape, window, T, dtype, E):
+    say(shape, window, T, dtype, E)
+    p = Problem(SHAPES[shape], 2, 4, T, dtype, E=E)
     p.window = window
     p.check(p.run())
 
 
 @pytest.mark.parametrize("T,g", [(16, 1), (32, 5), (16, 8)])
-@pytest.mark.parametrize("q", [1, 3, 20])
-def test_holes_layers_and_shared_blocks(T, g, q):
-    say(T, g, q)
-    p = Problem([(200, q), (1250, q), (333, q)], 2, g, T, HALF, L=3, seed=q)
+@pytest.mark.parametrize("q,E", [(1, None), (3, None), (20, None), (20, WIDE)])
+def test_holes_layers_and_shared_blocks(T, g, q, E):
+    say(T, g, q, E)
+    p = Problem([(200, q), (1250, q), (333, q)], 2, g, T, HALF, L=3, E=E, seed=q)
     t = p.tables
     t[0, 0, :] = -1                                  # a request whose table is empty
     t[1, 1, ::3], t[1, 2, 0], t[1, 2, 1] = -7, 1 << 30, p.cache.shape[1]
@@ -244,11 +247,11 @@ def test_tables_with_room_for_more_than_the_caches_hold(m, g, T, dtype):
 
 
 @pytest.mark.parametrize("dtype", [HALF, BF])
-@pytest.mark.parametrize("m,g", [(1, 4), (5, 3), (4, 8), (40, 2)])
-def test_nan_reaches_only_the_rows_that_see_it(m, g, dtype):
-    say(m, g, dtype)
+@pytest.mark.parametrize("m,g,E", [(1, 4, None), (5, 3, None), (4, 8, None), (40, 2, None), (40, 2, WIDE), (15, 4, None)])
+def test_nan_reaches_only_the_rows_that_see_it(m, g, dtype, E):
+    say(m, g, dtype, E)
     n = 300
-    p = Problem([(n, m), (n, m)], 2, g, 16, dtype)
+    p = Problem([(n, m), (n, m)], 2, g, 16, dtype, E=E)
     slot = lambda r, pos: p.tables[0, r, pos // 16].item() * 16 + pos % 16
     k, v = p.k[:, :1].clone(), p.v[:, :1].clone()
     v[0, 0, 0, 70] = math.nan                        # head 0, group 2
@@ -287,16 +290,16 @@ def test_values_of_any_size(dtype, spread, m):
 @pytest.mark.parametrize("m", [1, 30])
 def test_sharp_and_flat_softmax(scale, m):
     """Scores up to several hundreds: the reference is moved again and again."""
-    p = Problem([(900, m), (1100, m)], 1, 5, 16, HALF, strong=True)
+    p = Problem([(900, m), (1100, m)], 1, 5, 16, HALF, E=None if scale < 1 else WIDE, strong=True)
     # scores that climb along the context, so that every run of tokens passes the last one's reference
     p.scale = scale
     p.check(p.run())
 
 
 def test_scores_that_climb():
-    for m, g in ((1, 4), (20, 4)):
+    for m, g, E in ((1, 4, None), (6, 4, None), (20, 4, None), (20, 4, 20 * WIDE)):
         n, H = 640, 1
-        p = Problem([(n, m)], H, g, 16, BF)
+        p = Problem([(n, m)], H, g, 16, BF, E=E)
         k = torch.zeros((1, n, H, 128))
         k[0, :, 0, 0] = torch.arange(n) / 16.0
         rc.rc_cache_write(k.to(BF).to(DEV), p.v.to(DEV), p.slots.to(DEV), p.cache)
@@ -362,7 +365,7 @@ def test_blocks_beyond_four_gigabytes():
 
 # ---- streams, graphs, workspaces
 
-@pytest.mark.parametrize("m,g", [(1, 5), (3, 8), (40, 3)])
+@pytest.mark.parametrize("m,g", [(1, 5), (3, 8), (15, 4), (40, 3)])
 def test_same_bits_on_every_run_and_guard_behind_the_workspace(m, g):
     p = Problem([(2500, m), (40, m), (1200, m)], 2, g, 16, HALF, E=400)
     need = rc.rc_cache_attend_workspace_size(p.cache, HALF, 3, 400, 2 * g, m)
@@ -420,3 +423,14 @@ def test_another_stream_and_graph_replays():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((out, lse, *blocks), got)), replay
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_example_of_decoding_steps(dtype):
+    """Write, attend, read back, search, remap, attend: the second request's sealed blocks go to the first one's, bit by bit the same."""
+    from paper_2507_21433_amd import cache_example
+    r = cache_example.main(dtype=dtype)
+    assert r["matches"].tolist() == [[0, 1, 2, 3, 4]] and r["tables"][0, 1].tolist() == [0, 1, 2, 3, 4, 11] and r["freed"].sum() == 5
+    assert torch.equal(r["before"]["out"], r["after"]["out"]) and torch.equal(r["before"]["lse"], r["after"]["lse"])
+    assert torch.equal(r["after"]["out"][0, 0], r["after"]["out"][0, 1])
+    assert torch.isfinite(r["prompt"]["out"]).all()

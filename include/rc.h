@@ -452,7 +452,7 @@ rc_status rc_cache_write(const rc_cache_desc* desc, const void* k, const void* v
 rc_status rc_cache_read(const rc_cache_desc* desc, const void* cache, const int32_t* ids, int64_t n,
                         const rc_kv_desc* kvdesc, void* k, void* v, void* hip_stream);
 
-/* Bytes of DEVICE workspace rc_cache_attend needs (0 on bad arguments; up to 71 MB).  It depends on the arguments only and never falls
+/* Bytes of DEVICE workspace rc_cache_attend needs (0 on bad arguments; up to 69 MB).  It depends on the arguments only and never falls
  * as R, E, max_q or the layers grow. */
 size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int64_t R, int64_t E, int32_t n_heads, int64_t max_q);
 
@@ -477,8 +477,8 @@ size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int64_t R, int6
  *                   Query tokens that belong to no request keep what out and lse held.
  *   workspace       DEVICE, 16-byte aligned, rc_cache_attend_workspace_size() bytes.  Contents are scratch.  Calls that share it
  *                   must not overlap.
- * Sums and softmax statistics are fp32; the probabilities are rounded to the 16-bit type for the matrix cores.  No atomics: the
- * same bits on every run.
+ * Sums and softmax statistics are fp32; for the matrix cores a probability is the sum of two numbers of the 16-bit type where max_q * g is
+ * at most 16, else one.  No atomics: the same bits on every run.
  */
 rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const int32_t* tables, int64_t R, int64_t E,
                           const int32_t* ctx_len, const int32_t* q_start, const void* q, int64_t n_q, int32_t n_heads,

@@ -1,5 +1,7 @@
 // rc_cache_write and rc_cache_read: K and V of tokens quantised into the slots of a paged 4-bit cache, and blocks read back
-// out of it into the layout that rc_block_norms and the searches take.  Both stream: 16 bits and 4.25 bits a value.
+// out of it into the layout that rc_block_norms and the searches take.  Both stream 16 bits and 4.25 bits a value and are bound by memory:
+// 64 layers of 2.1k tokens written in 149 us (0.72 GB, 4.8 TB/s), a pool of 32 layers x 1013 blocks of 32 tokens read in 923 us (5.4 GB, 5.8 TB/s;
+// a copy of 8 GB runs at 6.3).  Their smallest calls are a launch, 2 to 4 us.
 #include <hip/hip_runtime.h>
 
 #include "rc_cache.hpp"
@@ -126,7 +128,8 @@ struct ReadArgs {
 };
 
 // A wave takes a record; lane (q, i) writes dims 8i .. 8i+7 of tokens 4q .. 4q+3: 256 consecutive bytes of a token per 16 lanes,
-// and the waves of a workgroup are neighbouring heads.
+// and the waves of a workgroup are neighbouring heads.  The values go out without being kept in the caches: 986 us instead of 948 for the pool
+// with ordinary stores.  (Four tokens of four heads to a wave, 1024 consecutive bytes at a time: 969.)
 template <bool BF16>
 __global__ __launch_bounds__(kCacheThreads) void cache_read_kernel(ReadArgs a) {
   const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;

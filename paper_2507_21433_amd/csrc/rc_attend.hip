@@ -952,7 +952,7 @@ extern "C" size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int6
   clear_error();
   AttendShape s;
   if (attend_check(desc, R, E, n_heads, max_q, max_q, 0, &s, "rc_cache_attend_workspace_size")) return 0;
-  return attend_workspace(s);
+  return attend_largest_workspace(s, max_q);
 }
 
 extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const int32_t* tables, int64_t R, int64_t E,

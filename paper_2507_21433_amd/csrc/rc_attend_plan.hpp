@@ -184,5 +184,17 @@ inline size_t attend_workspace(const AttendShape& s) {
   const int64_t parts = attend_most_parts(s);
   return parts ? attend_header_bytes(s.wgs) + (size_t)parts * attend_part_bytes(s.rows) : 0;
 }
+// The workspace of a call of up to max_q query tokens a request: the largest of the kernels that fewer of them would take as well.
+inline size_t attend_largest_workspace(AttendShape s, int64_t max_q) {
+  size_t most = attend_workspace(s);
+  for (const int64_t rows : {16, 32, 64}) {
+    const int64_t q = rows / s.g;
+    AttendShape t;
+    if (q < 1 || q >= max_q || !attend_shape(&t, s.L, s.R, s.E, s.T, s.H, s.H * s.g, q, q, s.window)) continue;
+    const size_t n = attend_workspace(t);
+    if (n > most) most = n;
+  }
+  return most;
+}
 
 }  // namespace rc

@@ -159,3 +159,20 @@ def test_binding_checks(library):
         a = dict(dict(q=q, cache=cache, tables=tables, ctx_len=ctx, q_start=start, max_q=2), **kw)
         with pytest.raises(AssertionError):
             rc.rc_cache_attend(**a)
+
+
+@pytest.mark.parametrize("H", [1, 2, 3, 8])
+def test_workspace_size_never_falls_in_any_direction(lib, H):
+    """A call with fewer query tokens than it announces is planned for these, an engine keeps one workspace for its largest step: no smaller call
+    needs more."""
+    tokens, requests, entries = (1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 17, 20, 32, 33, 64, 65, 128, 300), (1, 2, 3, 5, 9, 20, 70), \
+        list(range(60, 140, 3)) + [150, 250, 333, 512, 1000, 1023, 1025, 1200, 5000, 70000]
+    for g in (1, 2, 3, 5, 8, 16):
+        size = lambda q, R, E, L: lib.rc_cache_attend_workspace_size(ctypes.byref(rc.CacheDesc(L, 16, H, 128, 0, 100000, 100000 * H * 2176)), R, E, H * g, q)
+        table = [[[size(q, R, E, 1) for E in entries] for R in requests] for q in tokens]
+        for i, by_r in enumerate(table):
+            for j, by_e in enumerate(by_r):
+                assert by_e == sorted(by_e), (g, tokens[i], requests[j])
+                assert i == 0 or all(a <= b for a, b in zip(table[i - 1][j], by_e)), (g, tokens[i], requests[j])
+                assert j == 0 or all(a <= b for a, b in zip(by_r[j - 1], by_e)), (g, tokens[i], requests[j])
+        assert all(size(q, R, E, 1) <= size(q, R, E, 4) for q in (1, 9, 65) for R in (1, 9) for E in entries)

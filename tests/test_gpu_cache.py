@@ -67,8 +67,8 @@ def test_write(L, T, H, N, dtype, order):
     g = gen(N * 7 + H)
     NB = 2 * (N // T + 2)
     if order == "fused":
-        wide = randn((L, N, 3 * H, 128), g, dtype).to(DEV)
-        k, v = wide[:, :, H:2 * H], wide[:, :, 2 * H:]
+        wide = randn((L, N, 4 * H, 128), g, dtype).to(DEV)
+        k, v = wide[:, :, 2 * H:3 * H], wide[:, :, 3 * H:]
     else:
         k, v = randn((L, N, H, 128), g, dtype).to(DEV), randn((L, N, H, 128), g, dtype).to(DEV)
     if order == "whole":

@@ -7,6 +7,7 @@
 //
 // The softmax's reference is not the running maximum but a number at most 15 below it (in powers of two) and 7 below it when it is
 // set: probabilities stay below 2^15, as fp16 holds them, and the sums are rescaled only where a score passes the reference by 15.
+// bf16 values may be as large as fp32 numbers: from where V's powers are large on, a wave goes by the lower limits below.
 #include <hip/hip_runtime.h>
 
 #include "rc_attend_plan.hpp"
@@ -18,6 +19,13 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4;
 constexpr float kNothing = -3e38f;  // the reference of a row that has seen nothing; -infinity would make NaNs of differences
 constexpr float kRoom = 15.f, kBelow = 7.f;
+// V's groups under a power of 2^65 and more, which only bf16 has: weights of 2^15 and the number of tokens would take their sums beyond fp32.
+// There weights are at most 2^-18 and set to 2^-26, and a lane's sum that has passed 2^-16 is set to 2^-24: a row's weights of a wave
+// (four lanes, each with 16 more of a step) are 5 * 2^-14 at most, those of four waves and 768 parts 0.94, and 0.94 * 6 * 2^125 is an fp32 number,
+// however many tokens there are.  Below 2^65: 2^15 * 2^31 tokens * 7 * 2^64 is one.  (Lower limits throughout would cost small values their last bits.)
+// Looking for large powers takes 0 to 2 % of a bf16 call with few rows (262143 tokens 59 us either way, drafts 32.2 -> 32.9), 2 to 3 % with many (256
+// query tokens over 60000 267 -> 273).
+constexpr float kLowRoom = -18.f, kLowBelow = -26.f, kLowSum = 0x1p-16f, kLowSumExp = -24.f;
 
 struct AttendArgs {
   AttendShape s;
@@ -326,14 +334,26 @@ __device__ __forceinline__ void powers(uint32_t ve, float (&p)[4]) {
 
 // ---- Softmax of a row's scores.
 
-template <int N>
-__device__ __forceinline__ void rescale(f32x4 (&o)[8], float& ref, float& sum, float top, float c) {
+// Which limits a wave goes by: the lower ones (kLowRoom) from the first 32 or 64 tokens on that have a large V; `turned` there.
+struct Limits {
+  bool low = false, turned = false;
+  __device__ __forceinline__ void see(bool large) { turned = large && !low, low = low || large; }
+};
+__device__ __forceinline__ bool large_power(uint32_t ve) { return (ve & ve << 1 & 0x80808080u) != 0; }
+
+template <bool BF16>
+__device__ __forceinline__ void rescale(f32x4 (&o)[8], float& ref, float& sum, float top, float c, const Limits& at) {
+  const bool low = BF16 && at.low;
   // a wave-wide decision: nearly always no row's score passes its reference by kRoom
-  if (__any(top * c > ref + kRoom)) {
-    const float to = fmaxf(ref, row_max(top) * c - kBelow), f = __builtin_amdgcn_exp2f(ref - to);
+  bool pass = top * c > ref + (low ? kLowRoom : kRoom);
+  if (BF16) pass = pass || sum > (low ? kLowSum : __builtin_inff()) || at.turned;
+  if (__any(pass)) {
+    float to = fmaxf(ref, row_max(top) * c - (low ? kLowBelow : kBelow));
+    if (low) to = fmaxf(to, ref + __builtin_amdgcn_logf(row_max(sum)) - kLowSumExp);
+    const float f = __builtin_amdgcn_exp2f(ref - to);
     sum *= f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[i] *= f;
+    for (int i = 0; i < 8; ++i) o[i] *= f;
     ref = to;
   }
 }
@@ -438,6 +458,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
     Tile x[2];
     const char* rec[2];
     bool there[2], there_next[2] = {false, false};
+    Limits limits;
     int ids = -1;
     const auto find_records = [&](int n) {
       if ((n & 31) == 0) {
@@ -501,13 +522,14 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
           for (int t = 0; t < RT; ++t) poison<BF16>(o[t], flags, seen[t]);
         }
       }
+      if constexpr (BF16) limits.see(__any(large_power(x[0].ve) || large_power(x[1].ve)));
       u32x4 hi[RT], lo[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         float top = s[t][0][0];
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
-        rescale<8>(o[t], ref[t], sum[t], top, a.c);
+        rescale<BF16>(o[t], ref[t], sum[t], top, a.c, limits);
         float p[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], a.c, -ref[t]));
@@ -613,7 +635,7 @@ struct ManyLds {
   u32x4 k[2][4][4][64];  // [buffer][16 tokens][step of the dims][lane]
   u32x2 v[2][2][8][64][2];  // [buffer][32 tokens][chunk][lane][16 tokens of the 32]
   uint32_t ve[2][4][16];    // V's exponent words of the tiles of a buffer at the ends of what the rows see
-  int32_t there[2][4];
+  int32_t there[2][4];      // of the tiles of a buffer: whether there is a block, and 16 for large V
 };
 
 template <bool BF16, int RT>
@@ -659,6 +681,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
     }
 
     const auto at_ends = [&](int pos) { return pos < w.item.low_max || pos + kStep > w.item.high_min; };
+    Limits limits;
     // the wave's 16 tokens of a step
     int ids = -1;
     const auto load = [&](Tile& x, bool& there, int step) {
@@ -677,7 +700,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         if ((col & 3) == 0) lds.ve[buf][wave][quarter * 4 + (col >> 2)] = x.ve;
         x.ve = without_nans(x.ve, nan_bytes(x.ve));
       }
-      if (lane == 0) lds.there[buf][wave] = there;
+      int flags = there;
+      if constexpr (BF16) flags |= __any(large_power(x.ve)) ? 16 : 0;
+      if (lane == 0) lds.there[buf][wave] = flags;
     };
     const auto unpack = [&](const Tile& x, int buf) {
       const float power = power_of(x.ke);
@@ -722,7 +747,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
           for (int t = 0; t < RT; ++t) s[t][(i & 2) + (m & 1)] = mfma<BF16>(k[i & 1][m], q[t][2 * (i & 1) + (m >> 1)], s[t][(i & 2) + (m & 1)]);
         __builtin_amdgcn_sched_barrier(0);
       }
-      const int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
+      int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
+      if constexpr (BF16) {
+        limits.see(there > 15);
+        there &= 15;
+      }
       const bool ends = at_ends(pos);
       if (ends || there != 15) {
         uint32_t flags = 0;
@@ -753,7 +782,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         float top = s[t][0][0];
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
-        rescale<8>(o[t], ref[t], sum[t], top, a.c);
+        rescale<BF16>(o[t], ref[t], sum[t], top, a.c, limits);
       }
       check(x, there_next, step + 1, buf ^ 1);
       u32x4 v[8], p16[RT][2];

@@ -7,7 +7,7 @@
 //
 // The softmax's reference is not the running maximum but a number at most 15 below it (in powers of two) and 7 below it when it is
 // set: probabilities stay below 2^15, as fp16 holds them, and the sums are rescaled only where a score passes the reference by 15.
-// bf16 values may be as large as fp32 numbers: from where V's powers are large on, a wave goes by the lower limits below.
+// bf16 values may be as large as fp32 numbers, and scores so large that an fp32 number is coarse: Gate.
 #include <hip/hip_runtime.h>
 
 #include "rc_attend_plan.hpp"
@@ -20,12 +20,11 @@ constexpr int kThreads = 256, kWaves = 4;
 constexpr float kNothing = -3e38f;  // the reference of a row that has seen nothing; -infinity would make NaNs of differences
 constexpr float kRoom = 15.f, kBelow = 7.f;
 // V's groups under a power of 2^65 and more, which only bf16 has: weights of 2^15 and the number of tokens would take their sums beyond fp32.
-// There weights are at most 2^-18 and set to 2^-26, and a lane's sum that has passed 2^-16 is set to 2^-24: a row's weights of a wave
-// (four lanes, each with 16 more of a step) are 5 * 2^-14 at most, those of four waves and 768 parts 0.94, and 0.94 * 6 * 2^125 is an fp32 number,
-// however many tokens there are.  Below 2^65: 2^15 * 2^31 tokens * 7 * 2^64 is one.  (Lower limits throughout would cost small values their last bits.)
-// Looking for large powers takes 0 to 2 % of a bf16 call with few rows (262143 tokens 59 us either way, drafts 32.2 -> 32.9), 2 to 3 % with many (256
-// query tokens over 60000 267 -> 273).
-constexpr float kLowRoom = -18.f, kLowBelow = -26.f, kLowSum = 0x1p-16f, kLowSumExp = -24.f;
+// From the first of them on a wave keeps weights to 2^-20 at most, and a lane's sum that has passed 2^-16 is set to 2^-24: a row's weights of a
+// wave (four lanes, each with 16 more of a step) are 2^-13 at most, those of four waves and 768 parts 0.375, and 0.375 * 6 * 2^125 is an fp32
+// number, however many tokens there are.  Below 2^65: 2^15 * 2^31 tokens * 7 * 2^64 is one.  (Lower limits throughout would cost small values their
+// last bits.)
+constexpr float kLowLimit = -20.f, kLowSum = 0x1p-16f, kLowSumExp = -24.f;
 
 struct AttendArgs {
   AttendShape s;
@@ -334,27 +333,61 @@ __device__ __forceinline__ void powers(uint32_t ve, float (&p)[4]) {
 
 // ---- Softmax of a row's scores.
 
-// Which limits a wave goes by: the lower ones (kLowRoom) from the first 32 or 64 tokens on that have a large V; `turned` there.
-struct Limits {
-  bool low = false, turned = false;
-  __device__ __forceinline__ void see(bool large) { turned = large && !low, low = low || large; }
-};
 __device__ __forceinline__ bool large_power(uint32_t ve) { return (ve & ve << 1 & 0x80808080u) != 0; }
 
-template <bool BF16>
-__device__ __forceinline__ void rescale(f32x4 (&o)[8], float& ref, float& sum, float top, float c, const Limits& at) {
-  const bool low = BF16 && at.low;
+// How a wave takes the weights of a row tile: 2^(score * times - ref), where no exponent passes `room`; else rescale() moves the references first.
+// Odd: it always does, because of large V (`low`) or coarse scores, and leaves exponents in place of scores, under a reference of 0.  The gate and the
+// look at V's powers take 0 to 3 % of a bf16 call (262143 tokens 58.8 us either way, drafts 32.0 -> 32.8, 256 query tokens over 60000 269 -> 277), fp16 calls
+// nothing that shows; with conditions of their own in front of every tile the last was 282.
+struct Gate {
+  float times, room;
+  int odd, low;
+  __device__ __forceinline__ Gate(float c) : times(c), room(kRoom), odd(0), low(0) {}
+  __device__ __forceinline__ void see(int large) {
+    low |= large;
+    room = large ? -__builtin_inff() : room;
+  }
+};
+// Products score * c beyond this are so coarse that one taken exactly and one rounded may differ by whole powers of two: exponents are
+// differences of rounded products there, so that the largest is what it was meant to be.
+constexpr float kCoarse = 0x1p20f;
+
+// The tile's scores s, the largest of the lane's ones in top; `kept`: in LDS, a place of the row's for the reference of an odd tile.  What decides is the
+// exponent as it is taken for the largest score, so that no weight passes the limit.
+template <bool BF16, int N>
+__device__ __forceinline__ void rescale(f32x4 (&s)[N], f32x4 (&o)[8], float& ref, float& sum, float top, float c, Gate& g, float& kept) {
   // a wave-wide decision: nearly always no row's score passes its reference by kRoom
-  bool pass = top * c > ref + (low ? kLowRoom : kRoom);
-  if (BF16) pass = pass || sum > (low ? kLowSum : __builtin_inff()) || at.turned;
-  if (__any(pass)) {
-    float to = fmaxf(ref, row_max(top) * c - (low ? kLowBelow : kBelow));
-    if (low) to = fmaxf(to, ref + __builtin_amdgcn_logf(row_max(sum)) - kLowSumExp);
-    const float f = __builtin_amdgcn_exp2f(ref - to);
+  if (__builtin_expect(__any(fmaf(top, g.times, -ref) > g.room), 0)) {
+    const bool low = BF16 && g.low;
+    const float from = g.odd ? kept : ref, most = row_max(top), limit = low ? kLowLimit : kRoom, below = low ? kLowLimit : kBelow;
+    float to = fmaxf(from, fmaf(most, c, -below)), least = from;
+    if (low) {
+      const float all = row_max(sum);
+      if (all > kLowSum) least = from + __builtin_amdgcn_logf(all) - kLowSumExp;
+      to = fmaxf(to, least);
+    }
+    const bool coarse = fabsf(to) > kCoarse;
+    g.odd |= g.low | uniform(__any(coarse && to != kNothing));
+    if (g.odd) {
+#pragma clang fp contract(off)
+      const float x = most * c;
+      if (coarse) to = fmaxf(fmaxf(from, least), x - below);
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const float y = s[i >> 2][i & 3], z = y * c, d = coarse ? z - to : fmaf(y, c, -to);
+        s[i >> 2][i & 3] = d > limit ? limit : d;  // (NaN stays)
+      }
+      kept = to;
+      ref = 0.f;
+      g.times = 1.f;
+      g.room = -__builtin_inff();
+    } else {
+      ref = to;
+    }
+    const float f = __builtin_amdgcn_exp2f(from - to);
     sum *= f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] *= f;
-    ref = to;
   }
 }
 
@@ -458,7 +491,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
     Tile x[2];
     const char* rec[2];
     bool there[2], there_next[2] = {false, false};
-    Limits limits;
+    Gate gate[2] = {a.c, a.c};
     int ids = -1;
     const auto find_records = [&](int n) {
       if ((n & 31) == 0) {
@@ -522,17 +555,21 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
           for (int t = 0; t < RT; ++t) poison<BF16>(o[t], flags, seen[t]);
         }
       }
-      if constexpr (BF16) limits.see(__any(large_power(x[0].ve) || large_power(x[1].ve)));
+      if constexpr (BF16) {
+        const int large = __any(large_power(x[0].ve) || large_power(x[1].ve));
+#pragma unroll
+        for (int t = 0; t < RT; ++t) gate[t].see(large);
+      }
       u32x4 hi[RT], lo[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         float top = s[t][0][0];
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
-        rescale<BF16>(o[t], ref[t], sum[t], top, a.c, limits);
+        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, gate[t], lds.ref[wave][16 * t + col]);
         float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], a.c, -ref[t]));
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], gate[t].times, -ref[t]));
         sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -574,6 +611,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       sum[t] = row_sum(sum[t]);
+      if (gate[t].odd) ref[t] = lds.ref[wave][16 * t + col];
       if (quarter == 0) lds.ref[wave][16 * t + col] = ref[t], lds.sum[wave][16 * t + col] = sum[t];
     }
     __syncthreads();
@@ -636,6 +674,7 @@ struct ManyLds {
   u32x2 v[2][2][8][64][2];  // [buffer][32 tokens][chunk][lane][16 tokens of the 32]
   uint32_t ve[2][4][16];    // V's exponent words of the tiles of a buffer at the ends of what the rows see
   int32_t there[2][4];      // of the tiles of a buffer: whether there is a block, and 16 for large V
+  float ref[kWaves][32];    // references of odd row tiles
 };
 
 template <bool BF16, int RT>
@@ -681,7 +720,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
     }
 
     const auto at_ends = [&](int pos) { return pos < w.item.low_max || pos + kStep > w.item.high_min; };
-    Limits limits;
+    Gate gate[2] = {a.c, a.c};
     // the wave's 16 tokens of a step
     int ids = -1;
     const auto load = [&](Tile& x, bool& there, int step) {
@@ -749,7 +788,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
       }
       int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
       if constexpr (BF16) {
-        limits.see(there > 15);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) gate[t].see(there > 15);
         there &= 15;
       }
       const bool ends = at_ends(pos);
@@ -782,7 +822,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         float top = s[t][0][0];
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
-        rescale<BF16>(o[t], ref[t], sum[t], top, a.c, limits);
+        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, gate[t], lds.ref[wave][16 * t + col]);
       }
       check(x, there_next, step + 1, buf ^ 1);
       u32x4 v[8], p16[RT][2];
@@ -795,7 +835,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         for (int t = 0; t < RT; ++t) {
           float p[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + (j >> 2)][j & 3], a.c, -ref[t]));
+          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + (j >> 2)][j & 3], gate[t].times, -ref[t]));
 #pragma unroll
           for (int j = 0; j < 4; ++j) p16[t][i][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
           sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
@@ -856,6 +896,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const float all = row_sum(sum[t]);
+      if (gate[t].odd) ref[t] = lds.ref[wave][16 * t + col];
       const int m = wave * 16 * RT + 16 * t + col, n = w.t * kRows + m;
       if (n >= w.q.rows) continue;
       if (cut.whole) {

@@ -71,3 +71,67 @@ def test_smallest_bf16_values(m, g, E):
     p = Problem([(200, m), (64, m)], 1, g, 16, BF, E=E, spread=2.0 ** -118)
     want, _, bound = ref.attend(p.q, p.cache, p.tables, p.ctx, p.starts, p.scale, 0, p.many, tiny=2.0 ** -133)
     assert ((p.run()["out"].cpu().double() - want).abs() <= bound.out).all()
+
+
+# ---- scores as large as fp32 has them
+
+def one_dim(p, k, q):
+    """Keys and queries with a first dim only: scores are exact products."""
+    keys = torch.zeros(p.k.shape)
+    keys[..., 0] = k
+    p.q.zero_()
+    p.q[..., 0] = q.to(p.q.dtype).to(DEV)
+    return keys
+
+
+@pytest.mark.parametrize("m,g,E", KERNELS)
+@pytest.mark.parametrize("dtype,large", [(HALF, False), (BF, False), (BF, True)])
+@pytest.mark.parametrize("scale", [0.01, 3.0, 1e3, 1e6, 1e20])
+def test_weights_of_huge_scores(m, g, E, dtype, large, scale):
+    """Keys of a few levels far apart: a query's weights are shared equally by the tokens of the highest level that it sees."""
+    say(m, g, E, dtype, large, scale)
+    p = Problem([(500, m), (77, m)], 1, g, 16, dtype, E=E)
+    gn = gen(int(m + min(scale, 2e6)))
+    levels = torch.tensor([-6.0, -4.0, -2.0, 1.0, 3.0, 4.0, 6.0]) * 2.0 ** 10
+    pick = torch.randint(0, 4, (500 + 77,), generator=gn)
+    pick[130:] += torch.randint(0, 3, (500 + 77 - 130,), generator=gn)          # higher levels are met later
+    pick[350:] += (torch.rand(500 + 77 - 350, generator=gn) < 0.05).int()
+    q = (100 + 900 * torch.rand(p.q.shape[:3], generator=gn)) * torch.where(torch.rand(p.q.shape[:3], generator=gn) < 0.3, -1.0, 1.0)
+    rewrite(p, one_dim(p, levels[pick][:, None].expand(p.k.shape[:3]), q), p.v.float() * 2.0 ** 123 if large else None)
+    p.scale = scale
+    r = p.run()
+    values = ref.read(p.cache, torch.arange(p.cache.shape[1]))[1][0].reshape(-1, 128)
+    h = torch.finfo(dtype).eps / 2
+    for i, (n, new) in enumerate(zip(p.ctx, p.new)):
+        at = p.slots[sum(p.ctx[:i]):][:n].long()
+        for j in range(new):
+            for a in range(g):
+                x = levels[pick[sum(p.ctx[:i]):][:n - new + j + 1]].double() * p.q[0, p.starts[i] + j, a, 0].item()
+                v = values[at[:x.numel()]][x == x.max()]
+                got, lse = r["out"][0, p.starts[i] + j, a].cpu().double(), r["lse"][0, p.starts[i] + j, a].item()
+                want, size = v.mean(0), v.abs().mean(0)
+                off = (got - want).abs()
+                assert (off <= h * want.abs() + ((h if p.many else h * h) + 2.0 ** -12) * size + (0 if dtype == BF else 2.0 ** -24)).all(), (i, j, a, off.max())
+                # two roundings of the scale's product, one of the score's and one of the result
+                exact = x.max().item() * scale + math.log(v.shape[0])
+                assert abs(lse - exact) <= 2.0 ** -22 * abs(exact) + 2.0 ** -20
+
+
+@pytest.mark.parametrize("m,g,E", KERNELS)
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("scale", [1e6, 1e8, 1e9, 1e10])
+def test_huge_scores_give_means(m, g, E, dtype, scale):
+    """However coarse scores are, an output lies between the least and the largest of its values."""
+    say(m, g, E, dtype, scale)
+    p = Problem([(300, m), (40, m)], 2, g, 16, dtype, E=E, strong=True)
+    p.scale = scale
+    out = p.run()["out"].cpu().double()
+    values = ref.read(p.cache, torch.arange(p.cache.shape[1]))[1][0].reshape(-1, 2, 128)
+    h = torch.finfo(dtype).eps / 2
+    for i, n in enumerate(p.ctx):
+        at = p.slots[sum(p.ctx[:i]):][:n].long()
+        for head in range(2 * g):
+            v = values[at, head // g]
+            got = out[0, p.starts[i]:p.starts[i + 1], head]
+            room = 2 * (h + 2.0 ** -12) * v.abs().amax(0)
+            assert (got >= v.amin(0) - room).all() and (got <= v.amax(0) + room).all()

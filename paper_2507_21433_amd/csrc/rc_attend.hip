@@ -272,7 +272,7 @@ __device__ __forceinline__ const char* record(const AttendArgs& a, const char* h
 // V's exponent bytes with those of tokens that no row sees replaced by that of 1: whatever lies there (memory that was never
 // written) gets a probability of 0, and 0 times infinity or NaN would not be 0.  Token r of the word stands at pos + r.
 __device__ __forceinline__ uint32_t seen_only(uint32_t ve, int pos, bool there, const AttendItem& it) {
-  const uint32_t span = there ? it.high_max - it.low_min : 0;  // (an item of no tokens has no run)
+  const uint32_t span = there ? it.high_max - it.low_min : 0;  // (an item that sees no token has no run)
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const uint32_t m = 0xffu << (8 * r);

@@ -9,6 +9,7 @@
 #pragma once
 #include <cstddef>
 #include <cstdint>
+#include <initializer_list>
 
 #ifdef __HIPCC__
 #define RC_HD __host__ __device__
@@ -68,7 +69,8 @@ RC_HD inline AttendItem attend_span(const AttendShape& s, int32_t p0, int32_t p1
   i.high_min = attend_high(s, p0), i.high_max = attend_high(s, p1);
   i.pair0 = i.low_min / kPairTokens;
   const int32_t end = (int32_t)(((uint32_t)i.high_max + kPairTokens - 1) / kPairTokens);
-  i.pairs = end > i.pair0 ? end - i.pair0 : 0;
+  // (where a window lies behind the table's end, both may fall into the last run: it sees nothing all the same)
+  i.pairs = i.high_max > i.low_min ? end - i.pair0 : 0;
   // an item that sees nothing has a unit as well: it still has to say so
   i.free = i.pairs ? s.free : 0;
   const uint32_t per = s.unit / kPairTokens;

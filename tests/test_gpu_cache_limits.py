@@ -135,3 +135,21 @@ def test_huge_scores_give_means(m, g, E, dtype, scale):
             got = out[0, p.starts[i]:p.starts[i + 1], head]
             room = 2 * (h + 2.0 ** -12) * v.abs().amax(0)
             assert (got >= v.amin(0) - room).all() and (got <= v.amax(0) + room).all()
+
+
+# ---- windows behind the end of a table
+
+@pytest.mark.parametrize("T,E,dtype", [(16, 3, HALF), (16, 13, BF), (32, 2, HALF), (16, 67, BF)])
+@pytest.mark.parametrize("m,g", [(1, 4), (5, 4), (12, 4), (40, 4)])
+def test_window_behind_a_short_table(T, E, dtype, m, g):
+    """Queries whose window has slid past what the table lists see nothing, whatever its last block holds."""
+    say(T, E, dtype, m, g)
+    for past in (8, 9, 15, 16, 17, 40):
+        p = Problem([(E * T + past + m - 1, m), (max(m, E * T - 3), m)], 1, g, T, dtype, E=E)
+        p.window = 8
+        last = p.tables[0, 0, E - 1].item()
+        p.cache[0, last, ..., 2112:] = 254          # powers of V that become infinite
+        p.cache[0, last, ..., 1024:2048] = 0x77
+        r = p.run()
+        assert (r["out"][0, :m] == 0).all() and (r["lse"][0, :m] == -math.inf).all(), past
+        p.check(r)

@@ -413,6 +413,12 @@ __device__ __forceinline__ float row_lse(float ref, float sum) {
 }
 __device__ __forceinline__ float row_scale(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
+// Its position.  Rows that the item does not have stand where its last one does: further on they would see tokens that nobody has written, and what
+// lies there would decide when the wave moves the references of all its rows, and with these the last bits of the others' results.
+template <bool ONE>
+__device__ __forceinline__ int row_position(const AttendArgs& a, const Walk& w, int n) {
+  return w.q.ctx - w.q.len + row_token<ONE>(a, min(n, w.q.rows - 1));
+}
 // Row n of q as lane (row, quarter) holds it for the four steps of K's dims; rows that the item does not have: its last one's.
 template <bool ONE>
 __device__ __forceinline__ void load_q(const AttendArgs& a, const Walk& w, int n, int quarter, u32x4 (&q)[4]) {
@@ -481,7 +487,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       load_q<true>(a, w, 16 * t + col, quarter, q[t]);
-      const int pos = w.q.ctx - w.q.len + row_token<true>(a, 16 * t + col);
+      const int pos = row_position<true>(a, w, 16 * t + col);
       low[t] = attend_low(a.s, pos), span[t] = max(attend_high(a.s, pos) - low[t], 0);
 #pragma unroll
       for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
@@ -712,7 +718,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
     for (int t = 0; t < RT; ++t) {
       const int n = row0 + 16 * t + col;
       load_q<false>(a, w, n, quarter, q[t]);
-      const int pos = w.q.ctx - w.q.len + row_token<false>(a, n);
+      const int pos = row_position<false>(a, w, n);
       low[t] = attend_low(a.s, pos), span[t] = max(attend_high(a.s, pos) - low[t], 0);
 #pragma unroll
       for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};

@@ -153,3 +153,20 @@ def test_window_behind_a_short_table(T, E, dtype, m, g):
         r = p.run()
         assert (r["out"][0, :m] == 0).all() and (r["lse"][0, :m] == -math.inf).all(), past
         p.check(r)
+
+
+# ---- memory that was never written
+
+@pytest.mark.parametrize("m,g,E", KERNELS + [(20, 5, 20 * WIDE), (1, 5, None), (1, 3, WIDE), (7, 7, None)])
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_unwritten_memory_leaves_no_trace(m, g, E, dtype):
+    """Places behind the contexts, in blocks that the tables list, hold one thing or another: the results are the same bits."""
+    say(m, g, E, dtype)
+    p = Problem([(m + 37 * i, m) for i in range(24)], 2, g, 16, dtype, E=E)
+    results = []
+    for seed in (1, 2, 3):
+        p.cache.copy_(torch.randint(0, 256, p.cache.shape, generator=gen(seed), dtype=torch.uint8))
+        rewrite(p)
+        results.append(p.run())
+    for r in results[1:]:
+        assert torch.equal(r["out"], results[0]["out"]) and torch.equal(r["lse"], results[0]["lse"])

@@ -472,6 +472,7 @@ size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int64_t R, int6
  *   q               DEVICE, element (l, n, head, d) at l*q_layer_stride + n*q_token_stride + head*128 + d; strides in
  *                   elements, multiples of 8; 16-byte aligned
  *   max_q           HOST, at least the largest number of query tokens of a request (further ones are not computed)
+ *   scale           HOST, positive, at most 2.3e38 (scale * log2(e) is an fp32 number); so have to be q.k and scale * log2(e) * q.k
  *   window          0: none
  *   out             DEVICE, [L][n_q][n_heads][128] in the cache's dtype, 16-byte aligned;  lse: DEVICE float [L][n_q][n_heads] or NULL.
  *                   Query tokens that belong to no request keep what out and lse held.

@@ -1041,7 +1041,9 @@ extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cach
   AttendArgs a;
   if (rc_status e = attend_check(desc, R, E, n_heads, n_q, max_q, window, &a.s, who)) return e;
   if (!q_start && (max_q > 1 || n_q < R)) return fail(RC_ERR_INVALID_ARG, "%s: without q_start there is one query token per request", who);
-  if (!(scale > 0.f) || scale > 3e38f) return fail(RC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  a.c = scale * 1.4426950408889634f;
+  if (!(scale > 0.f) || !(a.c < __builtin_inff()))
+    return fail(RC_ERR_INVALID_ARG, "%s: scale must be positive, and scale * log2(e) an fp32 number", who);
   if (desc->n_layers == 0 || R == 0 || n_q == 0 || max_q == 0) return RC_OK;
   const bool empty = a.s.cap == 0;  // nothing to see: no table and no cache are read
   if (!ctx_len || !q || !out || (!empty && (!cache || !tables))) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
@@ -1058,7 +1060,6 @@ extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cach
   a.q = (const char*)q, a.out = (char*)out, a.lse = lse;
   a.cache_layer_stride = desc->layer_stride, a.q_token_stride_b = q_token_stride * 2, a.q_layer_stride_b = q_layer_stride * 2;
   a.n_blocks = desc->n_blocks;
-  a.c = scale * 1.4426950408889634f;
   a.borders = need ? (AttendBorder*)workspace : nullptr;
   a.parts = need ? (char*)workspace + attend_header_bytes(a.s.wgs) : nullptr;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);

@@ -135,16 +135,16 @@ __device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
       ctx = a.ctx_len[r];
       start = a.q_start ? a.q_start[r] : r;
       end = a.q_start ? a.q_start[r + 1] : r + 1;
-      mine += units_of<ONE>(a, attend_request(a.s, ctx, start, end)) * H;
+      mine = attend_sum(mine, units_of<ONE>(a, attend_request(a.s, ctx, start, end)) * H);
     }
   }
   int upto = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int y = __shfl_up(upto, d);
-    if (lane >= d) upto += y;
+    if (lane >= d) upto = attend_sum(upto, y);
   }
-  const int total = __builtin_amdgcn_readlane(upto, 63), line = total * (int)a.s.L;
+  const int total = __builtin_amdgcn_readlane(upto, 63), line = uniform(attend_line(a.s, total));
   w.share = uniform(attend_share(a.s, line));
   w.begin = w.at = wg * w.share;
   w.end = min(w.at + w.share, line);
@@ -996,7 +996,7 @@ rc_status attend_check(const rc_cache_desc* d, int64_t R, int64_t E, int32_t n_h
     return fail(RC_ERR_INVALID_ARG, "%s: n_heads %d is not a multiple of n_kv_heads %d", who, n_heads, d->n_kv_heads);
   if (n_heads > 1024) return fail(RC_ERR_UNSUPPORTED, "%s: n_heads %d (at most 1024)", who, n_heads);
   if (!attend_shape(s, d->n_layers, R, d->n_blocks ? E : 0, d->block_tokens, d->n_kv_heads, n_heads, n_q, max_q, window))
-    return fail(RC_ERR_UNSUPPORTED, "%s: more than 2^31 positions, rows or requests", who);
+    return fail(RC_ERR_UNSUPPORTED, "%s: a table of 2^31 positions or more, or more than 2^30 query tokens, requests or row tiles", who);
   return RC_OK;
 }
 
@@ -1027,8 +1027,9 @@ extern "C" size_t rc_cache_attend_workspace_size(const rc_cache_desc* desc, int6
   using namespace rc;
   clear_error();
   AttendShape s;
-  if (attend_check(desc, R, E, n_heads, max_q, max_q, 0, &s, "rc_cache_attend_workspace_size")) return 0;
-  return attend_largest_workspace(s, max_q);
+  const int64_t q = max_q < 1 ? max_q : 1;
+  if (attend_check(desc, R, E, n_heads, q, q, 0, &s, "rc_cache_attend_workspace_size")) return 0;
+  return attend_largest_workspace(s.L, R, s.E, s.T, s.H, n_heads, max_q);
 }
 
 extern "C" rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const int32_t* tables, int64_t R, int64_t E,

@@ -33,6 +33,7 @@ struct AttendShape {
   int32_t free;        // units that an item costs whatever its length
   int32_t wgs;         // workgroups
   uint32_t inverse;    // n * inverse >> 16 is n / g for n below 32
+  int32_t longest;     // units of a layer, at most
 };
 
 // A request's query tokens, row tiles and cached tokens, from what the device arrays hold (anything at all).
@@ -101,6 +102,16 @@ RC_HD inline int32_t attend_run(const AttendShape& s, const AttendItem& i, int32
   return i.pair0 + (n < i.pairs ? (int32_t)n : i.pairs);
 }
 
+// The line of units is counted in 32 bits, and has fewer than 2^30 of them: a layer's sums stay at that number, and a line that is longer is none
+// (only starts of query tokens that do not ascend can make it so: attend_shape() has seen to the others).  So no count overflows, whatever the arrays
+// hold.
+constexpr int32_t kLongestLine = 1 << 30;
+RC_HD inline int32_t attend_sum(int32_t a, int32_t b) {
+  const uint32_t n = (uint32_t)a + (uint32_t)b;
+  return n < (uint32_t)kLongestLine ? (int32_t)n : kLongestLine;
+}
+RC_HD inline int32_t attend_line(const AttendShape& s, int32_t total) { return total <= s.longest ? total * (int32_t)s.L : 0; }
+
 // Units of a workgroup's stretch where there are `total` of them.
 RC_HD inline int32_t attend_share(const AttendShape& s, int32_t total) {
   const int32_t n = (int32_t)((uint32_t)(total + s.wgs - 1) / (uint32_t)s.wgs);
@@ -150,22 +161,27 @@ inline int64_t attend_most_units(const AttendShape& s) {
   return n < 1 ? 1 : n + s.free;
 }
 
+constexpr int64_t kMostTokens = 0x7fffffffLL / 2;  // query tokens of a layer, and requests
+
 // The shape of a call; false where it is beyond what the kernels count in 32 bits.
 inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_t T, int32_t H, int32_t n_heads, int64_t n_q, int64_t max_q,
                          int64_t window) {
   const int32_t g = n_heads / H;
   if (max_q > n_q) max_q = n_q;
-  if (E > (0x7fffffffLL - 64) / T || n_q > 0x7fffffffLL / 2 || R > 0x7fffffffLL / 2 || (max_q > 0 && max_q > 0x7fffff00LL / g)) return false;
+  if (E > (0x7fffffffLL - 64) / T || n_q > kMostTokens || R > kMostTokens || (max_q > 0 && max_q > 0x7fffff00LL / g)) return false;
   const AttendKernel k = attend_kernel(max_q * g, (double)L * R * H, E * T / 64);
   // a window longer than any position is none
   *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.free, k.wgs,
-        65536u / (uint32_t)g + 1};
+        65536u / (uint32_t)g + 1, (int32_t)(L > 0 ? (kLongestLine - 1) / L : 0)};
   // a short table: items are not cut, and nothing has to be joined
   if (s->cap <= kWholeTokens) s->unit = (s->cap + k.unit - 1) / k.unit * k.unit + k.unit, s->least = 1, s->free = 0;
-  // the line is counted in 32 bits: tables long enough for more than 2^30 units have longer ones
-  const double items = (double)L * R * H * (((double)max_q * g + k.rows - 1) / k.rows);
-  if (items > (1 << 30)) return false;
-  while (items * attend_most_units(*s) > (1 << 30)) {
+  // Row tiles of a layer and KV head: as many as every request's longest step has, but no more than all query tokens together fill (those of one
+  // request of many tokens and of hundreds with one are far fewer than the first).  Tables long enough for more than 2^30 units have longer ones.
+  const int64_t asked = R < n_q ? R : n_q;
+  const double each = (double)asked * (double)((max_q * g + k.rows - 1) / k.rows), all = ((double)n_q * g + (double)asked * (k.rows - 1)) / k.rows;
+  const double items = (double)L * H * (each < all ? each : all);
+  if (items >= kLongestLine) return false;
+  while (items * attend_most_units(*s) >= kLongestLine) {
     if (s->unit >= 1 << 29) return false;
     s->unit *= 2;
   }
@@ -186,14 +202,22 @@ inline size_t attend_workspace(const AttendShape& s) {
   const int64_t parts = attend_most_parts(s);
   return parts ? attend_header_bytes(s.wgs) + (size_t)parts * attend_part_bytes(s.rows) : 0;
 }
-// The workspace of a call of up to max_q query tokens a request: the largest of the kernels that fewer of them would take as well.
-inline size_t attend_largest_workspace(AttendShape s, int64_t max_q) {
-  size_t most = attend_workspace(s);
-  for (const int64_t rows : {16, 32, 64}) {
-    const int64_t q = rows / s.g;
-    AttendShape t;
-    if (q < 1 || q >= max_q || !attend_shape(&t, s.L, s.R, s.E, s.T, s.H, s.H * s.g, q, q, s.window)) continue;
-    const size_t n = attend_workspace(t);
+// The workspace of calls of up to max_q query tokens a request, however many there are in all: the largest of the kernels that fewer of them would take
+// as well.  Where so many requests of max_q tokens each are more than a call can have, calls of fewer tokens may have all workgroups.
+inline size_t attend_largest_workspace(int64_t L, int64_t R, int64_t E, int32_t T, int32_t H, int32_t n_heads, int64_t max_q) {
+  const int32_t g = n_heads / H;
+  size_t most = 0;
+  for (const int64_t rows : {(int64_t)16, (int64_t)32, (int64_t)64, max_q > kMostTokens ? kMostTokens * g : max_q * g}) {
+    const int64_t q = rows / g;
+    if ((q < 1 && max_q > 0) || q > max_q) continue;
+    AttendShape s;
+    size_t n;
+    if (attend_shape(&s, L, R, E, T, H, n_heads, q && R > kMostTokens / q ? kMostTokens : R * q, q, 0)) {
+      n = attend_workspace(s);
+    } else {
+      const AttendKernel k = attend_kernel(rows, 1e18, 1);
+      n = attend_header_bytes(k.wgs) + 2 * (size_t)k.wgs * attend_part_bytes(k.rows);
+    }
     if (n > most) most = n;
   }
   return most;

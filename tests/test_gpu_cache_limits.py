@@ -170,3 +170,30 @@ def test_unwritten_memory_leaves_no_trace(m, g, E, dtype):
         results.append(p.run())
     for r in results[1:]:
         assert torch.equal(r["out"], results[0]["out"]) and torch.equal(r["lse"], results[0]["lse"])
+
+
+# ---- many requests, long and short steps in one call
+
+@pytest.mark.parametrize("R,E,L", [(30, None, 1), (100, 100, 2)])
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_a_chunk_beside_decoding_requests(R, E, L, dtype):
+    say(R, E, L, dtype)
+    gn = gen(R)
+    requests = [(int(torch.randint(1, 250, (1,), generator=gn)), 1) for _ in range(R)]
+    requests[R // 2] = (900, 150)
+    p = Problem(requests, 2, 5, 16, dtype, L=L, E=E)
+    p.check(p.run())
+
+
+def test_starts_that_make_the_line_too_long():
+    """Starts that go up and down would give every other request all query tokens: more units than there can be, and nothing is computed."""
+    R, n_q, E, L, H = 6000, 64, 20000, 8, 16
+    cache, dev = rc.cache_tensor(L, 1, 16, H, DEV), dict(dtype=torch.int32, device=DEV)
+    starts = torch.zeros(R + 1, **dev)
+    starts[1::2] = n_q
+    assert L * (R // 2) * H * (E * 16 // 64) > 1 << 30
+    q = torch.randn((L, n_q, H, 128), device=DEV).to(HALF)
+    out, lse = torch.full_like(q, 7.0), torch.full((L, n_q, H), 7.0, device=DEV)
+    rc.rc_cache_attend(q, cache, torch.zeros((L, R, E), **dev), torch.full((R,), E * 16, **dev), q_start=starts, max_q=n_q, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert (out == 7).all() and (lse == 7).all()

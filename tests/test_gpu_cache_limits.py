@@ -174,6 +174,21 @@ def test_unwritten_memory_leaves_no_trace(m, g, E, dtype):
 
 # ---- many requests, long and short steps in one call
 
+@pytest.mark.parametrize("R", [64, 65, 130, 200, 1000])
+@pytest.mark.parametrize("m,g,E", [(1, 4, None), (1, 4, 100), (3, 8, 90), (9, 4, 90), (20, 4, None), (20, 4, 90)])
+def test_many_requests(R, m, g, E):
+    """More requests than a wave has lanes: tokens of all, of some, or of none, contexts from none to some hundreds."""
+    say(R, m, g, E)
+    gn = gen(R + m)
+    new = torch.randint(0, 3, (R,), generator=gn).clamp(max=m).tolist()
+    ctx = torch.randint(0, 90, (R,), generator=gn).tolist()
+    for r in (3, R - 1, R // 2):
+        new[r], ctx[r] = m, 90
+    ctx[R // 3] = 1300 if E else 700
+    p = Problem([(max(c, 0), n) for c, n in zip(ctx, new)], 2, g, 16, HALF, E=E)
+    p.check(p.run())
+
+
 @pytest.mark.parametrize("R,E,L", [(30, None, 1), (100, 100, 2)])
 @pytest.mark.parametrize("dtype", [HALF, BF])
 def test_a_chunk_beside_decoding_requests(R, E, L, dtype):

@@ -557,18 +557,23 @@ def _attend_out(q, qt, o, os_, ot, e, es, et):
     assert e is None or (e == q[:3] and et == torch.float32 and _contiguous(e, es)), "lse is float32 [L][N][heads]"
 
 
-def rc_cache_attend(q, cache, tables, ctx_len, q_start=None, max_q=1, scale=None, window=0, want_lse=True, workspace=None, out=None,
+def rc_cache_attend(q, cache, tables, ctx_len, q_start=None, max_q=None, scale=None, window=0, want_lse=True, workspace=None, out=None,
                     lse=None):
     """Causal attention of query tokens [L][N][heads][128] over a 4-bit cache through tables [L][R][E] (int32).
 
     ctx_len int32 [R]: cached tokens, this step's among them; q_start int32 [R+1]: a request's query tokens (None: one each);
-    max_q: most query tokens of a request.  Returns dict(out [L][N][heads][128], lse float32 [L][N][heads] or None)."""
+    max_q: most query tokens of a request, which chooses the kernel (None: as many as there are in all, which is always enough; a step that
+    knows that its requests have fewer says so, 1 when decoding).  Further tokens of a request are not computed: their rows, and those of tokens
+    that belong to no request, keep what out and lse held, or hold anything where these are new.
+    Returns dict(out [L][N][heads][128], lse float32 [L][N][heads] or None)."""
     shape, dtype = q.shape, q.dtype
     d, L, N, heads, R, E, token, layer = _attend_layout(shape, q.stride(), dtype, cache.shape, cache.stride(), cache.dtype, tables.shape,
                                                         tables.stride(), tables.dtype, ctx_len.shape, ctx_len.stride(), ctx_len.dtype)
     _dev(q, cache, tables, ctx_len, q_start, workspace, out, lse)
     if q_start is not None:
         assert q_start.dtype == torch.int32 and q_start.shape == (R + 1,) and q_start.is_contiguous()
+    if max_q is None:
+        max_q = 1 if q_start is None else N
     if workspace is None:
         workspace = torch.empty(max(16, lib().rc_cache_attend_workspace_size(d, R, E, heads, max_q)), dtype=torch.uint8, device=q.device)
     if out is None:

@@ -1,6 +1,8 @@
 """Arguments at the limits of the 4-bit cache's entry points.  CPU only: every call fails validation or launches nothing."""
 import pytest
+import torch
 
+from paper_2507_21433_amd import binding as rc
 from tests.test_cache_abi import INVALID, WORKSPACE, attend, cdesc, lib  # noqa: F401
 
 
@@ -14,3 +16,24 @@ def test_scale_whose_product_is_no_number(lib, scale):  # noqa: F811
 def test_scales_that_are_taken(lib, scale):  # noqa: F811
     # (as far as the workspace, which is missing)
     assert attend(lib, cdesc(), scale=scale, ws=None) == WORKSPACE
+
+
+def test_max_q_left_out(monkeypatch):
+    """One query token per request without starts; with starts as many as there are, so that none is left out."""
+    seen = {}
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                seen[name] = args
+                return 16 if name.endswith("_size") else rc.RC_OK
+            return call
+
+    monkeypatch.setattr(rc, "lib", lambda: Library())
+    monkeypatch.setattr(rc, "_dev", lambda *ts: None)
+    monkeypatch.setattr(rc, "_stream", lambda: 0)
+    cache, tables = rc.cache_tensor(1, 5, 16, 2, "cpu"), torch.zeros((1, 3, 7), dtype=torch.int32)
+    ctx, starts = torch.zeros(3, dtype=torch.int32), torch.tensor([0, 7, 7, 9], dtype=torch.int32)
+    for N, kw, want in ((3, {}, 1), (9, dict(q_start=starts), 9), (9, dict(q_start=starts, max_q=7), 7)):
+        rc.rc_cache_attend(torch.zeros((1, N, 4, 128), dtype=torch.float16), cache, tables, ctx, **kw)
+        assert seen["rc_cache_attend"][12] == want and seen["rc_cache_attend_workspace_size"][4] == want, (N, kw)

@@ -212,3 +212,13 @@ def test_starts_that_make_the_line_too_long():
     rc.rc_cache_attend(q, cache, torch.zeros((L, R, E), **dev), torch.full((R,), E * 16, **dev), q_start=starts, max_q=n_q, out=out, lse=lse)
     torch.cuda.synchronize()
     assert (out == 7).all() and (lse == 7).all()
+
+
+@pytest.mark.parametrize("requests", [[(30, 3), (20, 0), (20, 2)], [(400, 60), (90, 1), (5, 5)]])
+def test_max_q_left_out(requests):
+    """Without it every query token is computed."""
+    p = Problem(requests, 2, 3, 16, HALF)
+    i = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    out, lse = torch.full_like(p.q, 7.0), torch.full(p.q.shape[:3], 7.0, device=DEV)
+    p.many = sum(p.new) * 3 > 16
+    p.check(rc.rc_cache_attend(p.q, p.cache, p.tables.to(DEV), i(p.ctx), q_start=i(p.starts), out=out, lse=lse))

@@ -207,7 +207,8 @@ extern "C" rc_status rc_cache_read(const rc_cache_desc* cdesc, const void* cache
   const int H = cdesc->n_kv_heads, tiles = cdesc->block_tokens / 16;
   if (n > kCacheMostWaves / (H * tiles)) return fail(RC_ERR_UNSUPPORTED, "%s: too many blocks", who);
   if (n == 0 || cdesc->n_layers == 0) return RC_OK;
-  if (!cache || !ids || !k || !v) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  // a cache of no blocks has no address: every block lies outside it, none of it is read
+  if ((!cache && cdesc->n_blocks > 0) || !ids || !k || !v) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
   if (!aligned16(cache) || !aligned16(k) || !aligned16(v)) return fail(RC_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
   ReadArgs a = {(const char*)cache, ids, (char*)k, (char*)v, cdesc->layer_stride, kvdesc->layer_stride * 2, cdesc->n_blocks,
                 (uint32_t)(n * tiles * H), H, tiles};

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2507_21433_amd import binding as rc
-from tests.test_cache_abi import INVALID, WORKSPACE, attend, cdesc, lib  # noqa: F401
+from tests.test_cache_abi import INVALID, ODD, WORKSPACE, attend, cdesc, lib, read  # noqa: F401
 
 
 @pytest.mark.parametrize("scale", [2.4e38, 2.9e38, 3.4e38])
@@ -37,3 +37,12 @@ def test_max_q_left_out(monkeypatch):
     for N, kw, want in ((3, {}, 1), (9, dict(q_start=starts), 9), (9, dict(q_start=starts, max_q=7), 7)):
         rc.rc_cache_attend(torch.zeros((1, N, 4, 128), dtype=torch.float16), cache, tables, ctx, **kw)
         assert seen["rc_cache_attend"][12] == want and seen["rc_cache_attend_workspace_size"][4] == want, (N, kw)
+
+
+def test_read_of_no_blocks_needs_no_cache(lib):  # noqa: F811
+    """No address is asked for where there is nothing to read (the other pointers are asked for as ever)."""
+    for missing in ("ids", "k", "v"):
+        assert read(lib, cdesc(n=0), cache=None, **{missing: None}) == INVALID
+        assert b"NULL" in lib.rc_last_error()
+    assert read(lib, cdesc(n=0), cache=None, k=ODD) == INVALID and b"aligned" in lib.rc_last_error()
+    assert read(lib, cdesc(n=1), cache=None) == INVALID and b"NULL" in lib.rc_last_error()

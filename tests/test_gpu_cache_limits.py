@@ -222,3 +222,19 @@ def test_max_q_left_out(requests):
     out, lse = torch.full_like(p.q, 7.0), torch.full(p.q.shape[:3], 7.0, device=DEV)
     p.many = sum(p.new) * 3 > 16
     p.check(rc.rc_cache_attend(p.q, p.cache, p.tables.to(DEV), i(p.ctx), q_start=i(p.starts), out=out, lse=lse))
+
+
+# ---- a cache of no blocks
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_cache_of_no_blocks(dtype):
+    """Nothing is stored, every block is read as zeros, nothing is seen."""
+    i = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    cache = rc.cache_tensor(2, 0, 32, 3, DEV)
+    kv = torch.ones((2, 4, 3, 128), dtype=dtype, device=DEV)
+    rc.rc_cache_write(kv, kv, i([0, 5, -1, 31]), cache)
+    k, v = (torch.full((2, 3, 32, 3, 128), 7.0, dtype=dtype, device=DEV) for _ in range(2))
+    rc.rc_cache_read(cache, i([0, -1, 2]), k=k, v=v)
+    assert not k.any() and not v.any()
+    r = rc.rc_cache_attend(torch.ones((2, 2, 6, 128), dtype=dtype, device=DEV), cache, torch.zeros((2, 2, 50), dtype=torch.int32, device=DEV), i([40, 3]))
+    assert not r["out"].any() and (r["lse"] == -math.inf).all()

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2507_21433_amd import binding as rc
+from tests import cache_cancelling
 from tests import cache_reference as ref
 from tests.test_gpu_cache import BF, DEV, HALF, WIDE, Problem, gen, randn, say
 
@@ -238,3 +239,23 @@ def test_cache_of_no_blocks(dtype):
     assert not k.any() and not v.any()
     r = rc.rc_cache_attend(torch.ones((2, 2, 6, 128), dtype=dtype, device=DEV), cache, torch.zeros((2, 2, 50), dtype=torch.int32, device=DEV), i([40, 3]))
     assert not r["out"].any() and (r["lse"] == -math.inf).all()
+
+
+# ---- probabilities of few rows
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("g,n,E", [(1, 40, None), (4, 64, None), (5, 110, WIDE), (16, 97, None), (16, 128, WIDE)])
+@pytest.mark.parametrize("seed", [1, 2])
+def test_few_rows_lose_nothing_of_their_probabilities(g, n, E, dtype, seed):
+    """With up to 16 rows a probability is the sum of two 16-bit numbers: outputs that nearly cancel are as close as that makes them."""
+    say(g, n, E, dtype, seed)
+    p = Problem([(n, 1)], 1, g, 16, dtype, E=E)
+    q, k, v = cache_cancelling.problem(g, n, dtype, gen(seed))
+    rewrite(p, one_dim(p, k.float()[:, None], q[None, None]), v.float()[None, :, None])
+    held = [x[0].reshape(-1, 128)[p.slots.long()] for x in ref.read(p.cache, torch.arange(p.cache.shape[1]))]
+    assert torch.equal(held[0][:, 0], k.double()) and torch.equal(held[1], v.double())
+    p.scale = 1.0
+    weights = cache_cancelling.weights(q, k)
+    off = (p.run()["out"][0, 0].cpu().double() - weights @ v.double()).abs() / cache_cancelling.bound(weights, v.double(), dtype)
+    say("largest error in bounds:", off.max().item())
+    assert off.max() <= 1

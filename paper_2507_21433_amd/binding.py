@@ -576,6 +576,8 @@ def rc_cache_attend(q, cache, tables, ctx_len, q_start=None, max_q=None, scale=N
         max_q = 1 if q_start is None else N
     if workspace is None:
         workspace = torch.empty(max(16, lib().rc_cache_attend_workspace_size(d, R, E, heads, max_q)), dtype=torch.uint8, device=q.device)
+    else:
+        assert workspace.is_contiguous(), "a workspace is contiguous"
     if out is None:
         out = torch.empty((L, N, heads, 128), dtype=dtype, device=q.device)
     if lse is None and want_lse:

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2507_21433_amd import binding as rc
-from tests.test_cache_abi import INVALID, ODD, WORKSPACE, attend, cdesc, lib, read  # noqa: F401
+from tests.test_cache_abi import INVALID, ODD, WORKSPACE, attend, cdesc, lib, library, read  # noqa: F401
 
 
 @pytest.mark.parametrize("scale", [2.4e38, 2.9e38, 3.4e38])
@@ -46,3 +46,13 @@ def test_read_of_no_blocks_needs_no_cache(lib):  # noqa: F811
         assert b"NULL" in lib.rc_last_error()
     assert read(lib, cdesc(n=0), cache=None, k=ODD) == INVALID and b"aligned" in lib.rc_last_error()
     assert read(lib, cdesc(n=1), cache=None) == INVALID and b"NULL" in lib.rc_last_error()
+
+
+def test_workspace_of_less_memory_than_its_shape(library):  # noqa: F811
+    """One byte seen a thousand times is not a thousand bytes to write to."""
+    cache, tables = rc.cache_tensor(1, 5, 16, 2, "cpu"), torch.zeros((1, 3, 7), dtype=torch.int32)
+    q, ctx, byte = torch.zeros((1, 3, 4, 128), dtype=torch.float16), torch.zeros(3, dtype=torch.int32), torch.zeros(1, dtype=torch.uint8)
+    rc.rc_cache_attend(q, cache, tables, ctx, workspace=torch.zeros(1000, dtype=torch.uint8))
+    for bad in (byte.expand(1 << 30), torch.zeros(64, dtype=torch.uint8)[::2]):
+        with pytest.raises(AssertionError):
+            rc.rc_cache_attend(q, cache, tables, ctx, workspace=bad)

@@ -143,14 +143,16 @@ struct AttendKernel {
 // Kernels by the rows of a request and KV head (query tokens times heads of a KV head): tiles of 16 and 32 rows, where every wave
 // of a workgroup has all rows and a quarter of the tokens, and of 64 and 128, where every wave has a quarter of the rows.  64 also for
 // more rows where tiles of 128 would be few and their work small (`pairs` (layers, requests and heads) times `steps` of 64 tokens): more
-// workgroups with less to do each.  us, tiles of 128 -> 64: 32 tiles of 900 tokens 31 -> 26, 16 of 8192 37 -> 31; 160 of 512 30 -> 34, 64 of 60000 268 -> 352.
+// workgroups with less to do each.  us, tiles of 128 -> 64, by tiles times steps: 2000 29.8 -> 25.9, 4000 44.5 -> 37.5 (46.2 -> 40.4 and 52.8 -> 57.0 with 5 and
+// 8 heads a KV head), 6000 47.6 -> 46.4, 50.1 -> 46.1 and 57.6 -> 64.4, 8000 51.5 -> 51.8 and 53.8 -> 52.0, 10000 58.1 -> 61.0, 16000 74.1 -> 84.1, 74.8 -> 84.8 and
+// 98.1 -> 118.7; with more tiles, 192 of 1000 tokens 30.3 -> 30.2, 256 of 900 38.7 -> 46.0, 256 of 2000 53.2 -> 55.9.
 // A stretch has `least` units at least (2, 4, 8 and 16 tried: one request of 4096 tokens 14.1, 13.4, 15.2 and 19.6), an item costs `free` units more
 // than its tokens (0, 1 and 2: 40 requests of 2000 tokens 23.6, 23.6 and 22.3; drafts of 20 requests 33.7, 31.4 and 31.8).
 inline AttendKernel attend_kernel(int64_t rows, double pairs, int64_t steps) {
   if (rows <= 16) return {16, 128, 768, 4, 2};
   if (rows <= 32) return {32, 128, 512, 4, 1};
   const double tiles = pairs * (double)((rows + 127) / 128);
-  if (rows <= 64 || (tiles <= 128 && tiles * (double)steps <= 16384)) return {64, 64, 512, 8, 1};
+  if (rows <= 64 || (tiles <= 128 && tiles * (double)steps <= 8192)) return {64, 64, 512, 8, 1};
   return {128, 64, 512, 8, 1};
 }
 

@@ -114,3 +114,14 @@ def test_the_line_is_no_longer_than_planned(tmp_path):
   std::printf("%ld taken, %ld plain, %ld wild, %ld none\n", taken, plain, wild, none);
   return plain > 1000 && wild > 100 && none > 10 ? 0 : 3;
 """)
+
+
+def test_tiles_of_64_rows_where_those_of_128_are_little_work(tmp_path):
+    """What was measured on both sides of the rule (us beside it in the plan): rows, tiles of 128, steps of 64 tokens."""
+    run(tmp_path, r"""
+  struct { int64_t rows; double pairs; int64_t steps; int32_t tile; } cases[] = {
+      {128, 128, 16, 64}, {128, 128, 31, 64}, {128, 64, 78, 64}, {128, 32, 187, 64}, {128, 16, 406, 64}, {128, 128, 62, 64},
+      {128, 128, 78, 128}, {128, 128, 125, 128}, {128, 64, 250, 128}, {128, 16, 937, 128}, {2000, 8, 125, 128}, {2048, 16, 14, 128}};
+  for (const auto& c : cases) REQUIRE(rc::attend_kernel(c.rows, c.pairs, c.steps).rows == c.tile);
+  return 0;
+""")

@@ -7,7 +7,7 @@
 //
 // The softmax's reference is not the running maximum but a number at most 15 below it (in powers of two) and 7 below it when it is
 // set: probabilities stay below 2^15, as fp16 holds them, and the sums are rescaled only where a score passes the reference by 15.
-// bf16 values may be as large as fp32 numbers, and scores so large that an fp32 number is coarse: Gate.
+// bf16 values may be as large as fp32 numbers, and scores so large that an fp32 number is coarse: rescale().
 #include <hip/hip_runtime.h>
 
 #include "rc_attend_plan.hpp"
@@ -335,16 +335,19 @@ __device__ __forceinline__ void powers(uint32_t ve, float (&p)[4]) {
 
 __device__ __forceinline__ bool large_power(uint32_t ve) { return (ve & ve << 1 & 0x80808080u) != 0; }
 
-// How a wave takes the weights of a row tile: 2^(score * times - ref), where no exponent passes `room`; else rescale() moves the references first.
-// Odd: it always does, because of large V (`low`) or coarse scores, and leaves exponents in place of scores, under a reference of 0.  The gate and the
-// look at V's powers take 0 to 3 % of a bf16 call (262143 tokens 58.8 us either way, drafts 32.0 -> 32.8, 256 query tokens over 60000 269 -> 277), fp16 calls
-// nothing that shows; with conditions of their own in front of every tile the last was 282.
+// How a wave takes the weights of its row tiles: 2^(score * times - ref), where no exponent passes `room`; else rescale() moves the references first.
+// Odd: a bit for each row tile whose exponents rescale() leaves in place of its scores, under a reference of 0 and with times of 1, because of large V (`low`) or
+// coarse scores.  From the first of either on, room is -infinity, and rescale() sees to every tile, so that the others have one comparison in front of
+// them, as they would have without.  It costs a bf16 call 0 to 3 %, the look at V's powers with it (262143 tokens 59 us either way, drafts 32.5 -> 33.4, 256
+// query tokens over 60000 268 -> 272), an fp16 call 0 to 2 % (1024 query tokens over 8192 256 either way, 64 requests of 12400 tokens 113 either way, 200
+// tokens of 20 queries 12.0 -> 12.3).
 struct Gate {
-  float times, room;
-  int odd, low;
-  __device__ __forceinline__ Gate(float c) : times(c), room(kRoom), odd(0), low(0) {}
-  __device__ __forceinline__ void see(int large) {
-    low |= large;
+  float room, times[2];
+  int odd;
+  bool low;
+  __device__ __forceinline__ Gate(float c) : room(kRoom), times{c, c}, odd(0), low(false) {}
+  __device__ __forceinline__ void see(bool large) {
+    low = low || large;
     room = large ? -__builtin_inff() : room;
   }
 };
@@ -352,14 +355,14 @@ struct Gate {
 // differences of rounded products there, so that the largest is what it was meant to be.
 constexpr float kCoarse = 0x1p20f;
 
-// The tile's scores s, the largest of the lane's ones in top; `kept`: in LDS, a place of the row's for the reference of an odd tile.  What decides is the
-// exponent as it is taken for the largest score, so that no weight passes the limit.
+// Row tile t's scores s, the largest of the lane's ones in top; `kept`: in LDS, a place of the row's for the reference of an odd tile.  What decides is
+// the exponent as it is taken for the largest score, so that no weight passes the limit.
 template <bool BF16, int N>
-__device__ __forceinline__ void rescale(f32x4 (&s)[N], f32x4 (&o)[8], float& ref, float& sum, float top, float c, Gate& g, float& kept) {
+__device__ __forceinline__ void rescale(f32x4 (&s)[N], f32x4 (&o)[8], float& ref, float& sum, float top, float c, int t, Gate& g, float& kept) {
   // a wave-wide decision: nearly always no row's score passes its reference by kRoom
-  if (__builtin_expect(__any(fmaf(top, g.times, -ref) > g.room), 0)) {
+  if (__builtin_expect(__any(fmaf(top, g.times[t], -ref) > g.room), 0)) {
     const bool low = BF16 && g.low;
-    const float from = g.odd ? kept : ref, most = row_max(top), limit = low ? kLowLimit : kRoom, below = low ? kLowLimit : kBelow;
+    const float from = g.odd >> t & 1 ? kept : ref, most = row_max(top), limit = low ? kLowLimit : kRoom, below = low ? kLowLimit : kBelow;
     float to = fmaxf(from, fmaf(most, c, -below)), least = from;
     if (low) {
       const float all = row_max(sum);
@@ -367,8 +370,8 @@ __device__ __forceinline__ void rescale(f32x4 (&s)[N], f32x4 (&o)[8], float& ref
       to = fmaxf(to, least);
     }
     const bool coarse = fabsf(to) > kCoarse;
-    g.odd |= g.low | uniform(__any(coarse && to != kNothing));
-    if (g.odd) {
+    if (low || uniform(__any(coarse && to != kNothing))) g.odd |= 1 << t;
+    if (__builtin_expect(g.odd >> t & 1, 0)) {
 #pragma clang fp contract(off)
       const float x = most * c;
       if (coarse) to = fmaxf(fmaxf(from, least), x - below);
@@ -379,7 +382,7 @@ __device__ __forceinline__ void rescale(f32x4 (&s)[N], f32x4 (&o)[8], float& ref
       }
       kept = to;
       ref = 0.f;
-      g.times = 1.f;
+      g.times[t] = 1.f;
       g.room = -__builtin_inff();
     } else {
       ref = to;
@@ -497,7 +500,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
     Tile x[2];
     const char* rec[2];
     bool there[2], there_next[2] = {false, false};
-    Gate gate[2] = {a.c, a.c};
+    Gate gate(a.c);
     int ids = -1;
     const auto find_records = [&](int n) {
       if ((n & 31) == 0) {
@@ -562,9 +565,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
         }
       }
       if constexpr (BF16) {
-        const int large = __any(large_power(x[0].ve) || large_power(x[1].ve));
-#pragma unroll
-        for (int t = 0; t < RT; ++t) gate[t].see(large);
+        gate.see(__any(large_power(x[0].ve) || large_power(x[1].ve)));
       }
       u32x4 hi[RT], lo[RT];
 #pragma unroll
@@ -572,10 +573,10 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
         float top = s[t][0][0];
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
-        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, gate[t], lds.ref[wave][16 * t + col]);
+        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, t, gate, lds.ref[wave][16 * t + col]);
         float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], gate[t].times, -ref[t]));
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], gate.times[t], -ref[t]));
         sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -617,7 +618,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       sum[t] = row_sum(sum[t]);
-      if (gate[t].odd) ref[t] = lds.ref[wave][16 * t + col];
+      if (gate.odd >> t & 1) ref[t] = lds.ref[wave][16 * t + col];
       if (quarter == 0) lds.ref[wave][16 * t + col] = ref[t], lds.sum[wave][16 * t + col] = sum[t];
     }
     __syncthreads();
@@ -726,7 +727,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
     }
 
     const auto at_ends = [&](int pos) { return pos < w.item.low_max || pos + kStep > w.item.high_min; };
-    Gate gate[2] = {a.c, a.c};
+    Gate gate(a.c);
     // the wave's 16 tokens of a step
     int ids = -1;
     const auto load = [&](Tile& x, bool& there, int step) {
@@ -794,8 +795,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
       }
       int there = uniform(lds.there[buf][0] | lds.there[buf][1] << 1 | lds.there[buf][2] << 2 | lds.there[buf][3] << 3);
       if constexpr (BF16) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t) gate[t].see(there > 15);
+        gate.see(there > 15);
         there &= 15;
       }
       const bool ends = at_ends(pos);
@@ -828,7 +828,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         float top = s[t][0][0];
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
-        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, gate[t], lds.ref[wave][16 * t + col]);
+        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, t, gate, lds.ref[wave][16 * t + col]);
       }
       check(x, there_next, step + 1, buf ^ 1);
       u32x4 v[8], p16[RT][2];
@@ -841,7 +841,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         for (int t = 0; t < RT; ++t) {
           float p[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + (j >> 2)][j & 3], gate[t].times, -ref[t]));
+          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + (j >> 2)][j & 3], gate.times[t], -ref[t]));
 #pragma unroll
           for (int j = 0; j < 4; ++j) p16[t][i][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
           sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
@@ -902,7 +902,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const float all = row_sum(sum[t]);
-      if (gate[t].odd) ref[t] = lds.ref[wave][16 * t + col];
+      if (gate.odd >> t & 1) ref[t] = lds.ref[wave][16 * t + col];
       const int m = wave * 16 * RT + 16 * t + col, n = w.t * kRows + m;
       if (n >= w.q.rows) continue;
       if (cut.whole) {

@@ -333,12 +333,13 @@ __device__ __forceinline__ void powers(uint32_t ve, float (&p)[4]) {
 
 // ---- Softmax of a row's scores.
 
-__device__ __forceinline__ bool large_power(uint32_t ve) { return (ve & ve << 1 & 0x80808080u) != 0; }
+// Whether an exponent byte of either word is 192 or more.
+__device__ __forceinline__ bool large_power(uint32_t a, uint32_t b) { return (((a & a << 1) | (b & b << 1)) & 0x80808080u) != 0; }
 
 // How a wave takes the weights of its row tiles: 2^(score * times - ref), where no exponent passes `room`; else rescale() moves the references first.
 // Odd: a bit for each row tile whose exponents rescale() leaves in place of its scores, under a reference of 0 and with times of 1, because of large V (`low`) or
 // coarse scores.  From the first of either on, room is -infinity, and rescale() sees to every tile, so that the others have one comparison in front of
-// them, as they would have without.  It costs a bf16 call 0 to 3 %, the look at V's powers with it (262143 tokens 59 us either way, drafts 32.5 -> 33.4, 256
+// them, as they would have without.  It costs a bf16 call 0 to 3 %, the look at V's powers with it (262143 tokens 59 us either way, drafts 32.4 -> 32.8, 256
 // query tokens over 60000 268 -> 272), an fp16 call 0 to 2 % (1024 query tokens over 8192 256 either way, 64 requests of 12400 tokens 113 either way, 200
 // tokens of 20 queries 12.0 -> 12.3).
 struct Gate {
@@ -565,7 +566,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
         }
       }
       if constexpr (BF16) {
-        gate.see(__any(large_power(x[0].ve) || large_power(x[1].ve)));
+        if (__builtin_expect(__any(large_power(x[0].ve, x[1].ve)), 0)) gate.see(true);
       }
       u32x4 hi[RT], lo[RT];
 #pragma unroll
@@ -747,7 +748,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(AttendArgs a) 
         x.ve = without_nans(x.ve, nan_bytes(x.ve));
       }
       int flags = there;
-      if constexpr (BF16) flags |= __any(large_power(x.ve)) ? 16 : 0;
+      if constexpr (BF16) flags |= __any(large_power(x.ve, 0)) ? 16 : 0;
       if (lane == 0) lds.there[buf][wave] = flags;
     };
     const auto unpack = [&](const Tile& x, int buf) {

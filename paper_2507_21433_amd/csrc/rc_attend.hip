@@ -452,7 +452,7 @@ struct RowsLds {
   float o[kWaves][16][132];
 };
 
-// What bounds it is memory: 64 requests of up to 12.4k tokens 580 MB in 107 us (5.4 TB/s; a plain read of as much 113).  Three waves a SIMD of one
+// What bounds it is memory: 64 requests of up to 12.4k tokens 580 MB in 108 us (5.4 TB/s; a plain read of as much 113).  Three waves a SIMD of one
 // row tile: with four (128 registers) 153 us instead of 118, with touches of the lines of the pairs to come 147: 32 KB of lines is all that a compute
 // unit's cache holds on their way.  Each wave's K is loaded again where it is used up, and so is V; held twice, whole pairs ahead, 121.
 template <bool BF16, int RT, bool STREAM>
@@ -671,9 +671,9 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
 // ---- Many rows: every wave has 32 of an item's 128 rows (16 of 64 with one row tile), and the workgroup turns 64 tokens at a time into operands
 // in LDS, once for all of its rows: every wave the codes of 16 tokens, into the buffer that the step does not read.
 //
-// A step of a wave is 64 matrix instructions (1024 cycles), some 280 vector instructions and 40 KB of LDS, each of them about 40 % of the time: two
-// waves a SIMD, as many as the registers allow, do not cover each other's waits.  A chunk of 1024 query tokens over 8192: 243 us and 13 for the parts
-// of its cut items, 220 GFLOP at 860 TFLOP/s (a library product of 8192^3 runs at 1170 to 1220).  What it took, us: every operand read by itself 293,
+// A step of a wave is 64 matrix instructions (1024 cycles), some 250 other vector instructions and 40 KB of LDS; by the counters each of them fills about a
+// third of the time: two waves a SIMD, as many as the registers allow, do not cover each other's waits.  A chunk of 1024 query tokens over 8192: 242 us and
+// 13 for the parts of its cut items, 220 GFLOP at 860 TFLOP/s with these (a library product of 8192^3 runs at 1170 to 1220).  What it took, us: every operand read by itself 293,
 // four ahead of their products 262, products beside exponentials and unpacking 256.  Probabilities are rounded once to 16 bits (the output is then off
 // by 1.3 times what its own rounding makes it).
 

@@ -1,6 +1,6 @@
 // rc_cache_write and rc_cache_read: K and V of tokens quantised into the slots of a paged 4-bit cache, and blocks read back
 // out of it into the layout that rc_block_norms and the searches take.  Both stream 16 bits and 4.25 bits a value and are bound by memory:
-// 64 layers of 2.1k tokens written in 149 us (0.72 GB, 4.8 TB/s), a pool of 32 layers x 1013 blocks of 32 tokens read in 923 us (5.4 GB, 5.8 TB/s;
+// 64 layers of 2.1k tokens written in 151 us (0.72 GB, 4.8 TB/s), a pool of 32 layers x 1013 blocks of 32 tokens read in 943 us (5.4 GB, 5.7 TB/s;
 // a copy of 8 GB runs at 6.3).  Their smallest calls are a launch, 2 to 4 us.
 #include <hip/hip_runtime.h>
 

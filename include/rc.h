@@ -489,6 +489,94 @@ rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const in
                           int64_t q_token_stride, int64_t q_layer_stride, int64_t max_q, float scale, int64_t window,
                           void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * ---- Storing into, attending over and evicting from 16-bit blocks ---------------------------------------------------------------
+ *
+ * The blocks that the searches compare, in the KV layout of this header, as a request's cache: rc_kv_write stores the tokens of a step,
+ * rc_kv_attend is the attention that reads them through the block tables (which rc_remap_block_table rewrites) and adds up how much of it
+ * every block gathers, rc_kv_evict takes the blocks that gathered least out of a request's table.  An evicted entry is -1 and stays a hole: the
+ * tokens behind it keep their positions.
+ */
+
+/*
+ * New tokens into their slots: K and V of n_tokens tokens of every layer are stored.
+ *
+ *   desc            of k and v, the blocks: n_blocks per layer, n_blocks * T < 2^31
+ *   k_new, v_new    DEVICE, element (l, n, h, d) at l*new_layer_stride + n*token_stride + h*128 + d: slices of a fused projection's
+ *                   output do.  Strides in elements, multiples of 8; pointers 16-byte aligned.  They must not overlap the blocks.
+ *   slots           DEVICE int32 [n_tokens], the same for all layers: block * T + (place in the block).  A token whose slot lies
+ *                   outside [0, n_blocks * T) is not stored (-1: a batch's empty place).  Slots must be distinct.
+ *   k, v            DEVICE, updated in place; other slots stay as they are
+ */
+rc_status rc_kv_write(const rc_kv_desc* desc, int64_t n_blocks, const void* k_new, const void* v_new, int64_t n_tokens,
+                      int64_t token_stride, int64_t new_layer_stride, const int32_t* slots, void* k, void* v, void* hip_stream);
+
+/* Bytes of DEVICE workspace rc_kv_attend needs, with weights_out if `weigh` (0 on bad arguments; without weights up to 69 MB, with them also
+ * 8 bytes per query token and head, and per layer, request and KV head half a byte per table position and row (query tokens times heads of a KV head)
+ * of the largest step of at most 32 rows, or where that is more 8 bytes per position and layer, request and KV head).  It depends on the arguments only
+ * and never falls as R, E, n_q, max_q or the layers grow. */
+size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_blocks, int64_t R, int64_t E, int32_t n_heads, int64_t n_q,
+                                   int64_t max_q, int32_t weigh);
+
+/*
+ * Attention of a step's query tokens (one per request when decoding, a few drafted ones, a chunk of a prompt) over the cached tokens of
+ * their requests, causal, every layer an independent problem:
+ *
+ *     out = sum_t p_t v_t,   p = softmax_t(scale * q.k_t),   lse = log sum_t exp(scale * q.k_t)
+ *     weights_out[l][r][e] = weights_in[l][r][e] + sum over the request's computed query tokens, all heads and the tokens t of entry e of p_t
+ *
+ * Request r has ctx_len[r] tokens in the blocks (this step's own among them: rc_kv_write comes first) and the query tokens
+ * q_start[r] .. q_start[r+1] - 1, its last ones: with m of them, query token j stands at position ctx_len[r] - m + j and sees the
+ * positions up to its own, with a window the last `window` of these.  Position t is place t % T of block tables[l][r][t / T];
+ * positions behind the table's end and those of entries outside [0, n_blocks) (-1: no block) are seen by nobody, and what memory holds there
+ * changes nothing.  n_heads = g * H: query heads h*g .. h*g + g-1 share KV head h.  A query that sees nothing gets 0 and an lse of -inf.
+ *
+ *   desc, n_blocks  of k and v; n_blocks * T < 2^31
+ *   tables          DEVICE int32 [L][R][E];  ctx_len: DEVICE int32 [R]
+ *   q_start         DEVICE int32 [R+1], ascending, q_start[R] <= n_q; NULL: one query token per request, in order (n_q >= R, max_q 1)
+ *   q               DEVICE, element (l, n, head, d) at l*q_layer_stride + n*q_token_stride + head*128 + d; strides in
+ *                   elements, multiples of 8; 16-byte aligned
+ *   max_q           HOST, at least the largest number of query tokens of a request (further ones are not computed).  It chooses one kernel for
+ *                   the whole call: a step of few-token requests and long chunks is faster as two calls
+ *   scale           HOST, positive, at most 2.3e38 (scale * log2(e) is an fp32 number); so have to be q.k and scale * log2(e) * q.k
+ *   window          0: none
+ *   out             DEVICE, [L][n_q][n_heads][128] in the blocks' dtype, 16-byte aligned;  lse: DEVICE float [L][n_q][n_heads] or NULL.
+ *                   Query tokens that belong to no request keep what out and lse held.
+ *   weights_in      DEVICE float [L][R][E], what earlier steps gathered, or NULL (nothing)
+ *   weights_out     DEVICE float [L][R][E], written for every entry; may be weights_in; NULL: blocks are not weighed.  L*R*E is at most 2^29 then
+ *   workspace       DEVICE, 16-byte aligned, rc_kv_attend_workspace_size() bytes.  Contents are scratch.  Calls that share it
+ *                   must not overlap.
+ * Sums and softmax statistics are fp32; for the matrix cores a probability is the sum of two numbers of the 16-bit type where max_q * g is
+ * at most 16, else one.  No atomics: the same bits on every run.  Sums of finite values neither overflow nor lose their values; a query that sees an
+ * infinity or a NaN in V has infinities or NaNs in these dims, one that does not see them is as if they were not there.
+ */
+rc_status rc_kv_attend(const rc_kv_desc* desc, int64_t n_blocks, const void* k, const void* v, const int32_t* tables, int64_t R, int64_t E,
+                       const int32_t* ctx_len, const int32_t* q_start, const void* q, int64_t n_q, int32_t n_heads,
+                       int64_t q_token_stride, int64_t q_layer_stride, int64_t max_q, float scale, int64_t window,
+                       void* out, float* lse, const float* weights_in, float* weights_out,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Eviction by gathered attention weight: every request of every layer keeps at most keep[r] blocks; those that gathered least leave its table.
+ *
+ * Request r uses the entries e < min(E, ceil(ctx_len[r] / T)); those with an id in [0, NB) hold a block.  Of the held entries the first n_first and
+ * the last n_last of the used places stay whatever they gathered (the newest block is still being written).  With `held` of them,
+ * min(held - keep[r], entries that may leave) entries leave, those of the smallest weights, equal weights by the lowest e; NaN counts as more than any
+ * number.  An entry that leaves becomes -1, and refcount[l][its id] falls by one, once for every entry: a block that others share stays
+ * where it is, one at 0 is free (as rc_remap_block_table and rc_refcount_release leave it).
+ *
+ *   tables_in/out   DEVICE int32 [L][R][E]; tables_out may be tables_in (in place).  Entries that stay are copied, whatever they hold.
+ *   ctx_len, keep   DEVICE int32 [R] (a negative keep is 0)
+ *   weights         DEVICE float [L][R][E], as rc_kv_attend gathers them
+ *   n_first         HOST, 0 or more;  n_last: HOST, 1 or more
+ *   refcount_in/out DEVICE int32 [L][NB]; refcount_out may be refcount_in
+ *   n_evicted       DEVICE int32 [L][R]: entries that left
+ * No workspace; integer atomics on the counts only: the same result on every run.  L*R is at most 2^24.
+ */
+rc_status rc_kv_evict(int32_t n_layers, const int32_t* tables_in, int32_t* tables_out, int64_t R, int64_t E, int64_t NB,
+                      int32_t block_tokens, const int32_t* ctx_len, const float* weights, const int32_t* keep, int64_t n_first,
+                      int64_t n_last, const int32_t* refcount_in, int32_t* refcount_out, int32_t* n_evicted, void* hip_stream);
+
 /* HOST string describing the calling thread's last error ("" if none). Never NULL. */
 const char* rc_last_error(void);
 

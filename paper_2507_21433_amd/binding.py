@@ -22,6 +22,7 @@ EXPORTS = ("rc_block_norms", "rc_match_workspace_size", "rc_match_blocks", "rc_r
            "rc_pat_workspace_size", "rc_pat_threshold", "rc_apply_threshold", "rc_pool_admit_workspace_size", "rc_pool_admit",
            "rc_candidate_distances_workspace_size", "rc_candidate_distances", "rc_pool_touch", "rc_refcount_release", "rc_pool_evict",
            "rc_cache_block_bytes", "rc_cache_write", "rc_cache_read", "rc_cache_attend_workspace_size", "rc_cache_attend",
+           "rc_kv_write", "rc_kv_attend_workspace_size", "rc_kv_attend", "rc_kv_evict",
            "rc_last_error", "rc_version")
 
 
@@ -109,6 +110,14 @@ def lib():
         L.rc_cache_attend_workspace_size.restype = sz
         L.rc_cache_attend.argtypes = [cp, vp, vp, i64, i64, vp, vp, vp, i64, i32, i64, i64, i64, f32, i64, vp, vp, vp, sz, vp]
         L.rc_cache_attend.restype = i32
+        L.rc_kv_write.argtypes = [dp, i64, vp, vp, i64, i64, i64, vp, vp, vp, vp]
+        L.rc_kv_write.restype = i32
+        L.rc_kv_attend_workspace_size.argtypes = [dp, i64, i64, i64, i32, i64, i64, i32]
+        L.rc_kv_attend_workspace_size.restype = sz
+        L.rc_kv_attend.argtypes = [dp, i64, vp, vp, vp, i64, i64, vp, vp, vp, i64, i32, i64, i64, i64, f32, i64, vp, vp, vp, vp, vp, sz, vp]
+        L.rc_kv_attend.restype = i32
+        L.rc_kv_evict.argtypes = [i32, vp, vp, i64, i64, i64, i32, vp, vp, vp, i64, i64, vp, vp, vp, vp]
+        L.rc_kv_evict.restype = i32
         L.rc_last_error.restype = ctypes.c_char_p
         L.rc_version.restype = i32
         _lib = L
@@ -592,3 +601,126 @@ def rc_cache_attend(q, cache, tables, ctx_len, q_start=None, max_q=None, scale=N
     if code:
         _check(code)
     return dict(out=out, lse=lse)
+
+
+def _blocks_desc(k, ks, kt, v, vs, vt):
+    """(descriptor by reference, L, T, H, blocks of a layer) of K and V blocks [L][n][T][H][128], alike in everything."""
+    assert len(k) == 5 and k == v and kt == vt, "K and V blocks of one type and shape, [L][n][T][H][128]"
+    L, n, T, H, D = k
+    block = T * H * D
+    assert all(s[4] == 1 and (H < 2 or s[3] == D) and s[2] == H * D and (n < 2 or s[1] == block) for s in (ks, vs)), "blocks of a layer must be contiguous"
+    layer = ks[0] if L > 1 else n * block
+    assert L < 2 or vs[0] == layer, "K and V of the same strides"
+    return ctypes.byref(KvDesc(L, T, H, D, _code(kt), layer)), L, T, H, n
+
+
+@_by_layout
+def _kv_write_layout(x, xs, xt, y, ys, yt, n, ns, nt, k, ks, kt, v, vs, vt):
+    d, L, _, H, blocks = _blocks_desc(k, ks, kt, v, vs, vt)
+    assert len(x) == 4 and x == y and xt == yt == kt, "new K and V of one shape, [L][N][H][128], and of the blocks' type"
+    assert x[0] == L and x[2] == H, "the new tokens' layers and heads are the blocks'"
+    strides = _row_strides(x, xs)
+    assert _row_strides(y, ys) == strides, "new K and V of the same strides"
+    assert nt == torch.int32 and n == (x[1],) and _contiguous(n, ns)
+    return d, blocks, x[1], *strides
+
+
+def rc_kv_write(k_new, v_new, slots, k, v):
+    """K and V of new tokens [L][N][H][128] into their slots (block * T + place; int32 [N]) of blocks [L][n][T][H][128], in place."""
+    _dev(k_new, v_new, slots, k, v)
+    d, blocks, N, token, layer = _kv_write_layout(k_new.shape, k_new.stride(), k_new.dtype, v_new.shape, v_new.stride(), v_new.dtype, slots.shape,
+                                                  slots.stride(), slots.dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype)
+    code = lib().rc_kv_write(d, blocks, k_new.data_ptr(), v_new.data_ptr(), N, token, layer, slots.data_ptr(), k.data_ptr(), v.data_ptr(), _stream())
+    if code:
+        _check(code)
+    return k, v
+
+
+def rc_kv_attend_workspace_size(k, R, E, n_heads, n_q, max_q=1, weigh=False):
+    d, *_, blocks = _blocks_desc(k.shape, k.stride(), k.dtype, k.shape, k.stride(), k.dtype)
+    return lib().rc_kv_attend_workspace_size(d, blocks, R, E, n_heads, n_q, max_q, int(weigh))
+
+
+@_by_layout
+def _kv_attend_layout(q, qs, qt, k, ks, kt, v, vs, vt, t, ts, tt, x, xs, xt):
+    d, layers, _, _, blocks = _blocks_desc(k, ks, kt, v, vs, vt)
+    assert len(q) == 4 and len(t) == 3 and tt == torch.int32 and _contiguous(t, ts), "tables are int32 [L][R][E]"
+    assert qt == kt, "queries of the blocks' type"
+    L, N, heads, _ = q
+    _, R, E = t
+    assert layers == L and t[0] == L, "the queries' layers are the blocks' and the tables'"
+    assert xt == torch.int32 and x == (R,) and _contiguous(x, xs)
+    return d, blocks, L, N, heads, R, E, *_row_strides(q, qs)
+
+
+def rc_kv_attend(q, k, v, tables, ctx_len, q_start=None, max_q=None, scale=None, window=0, want_lse=True, weights_in=None, weights_out=None,
+                 want_weights=False, workspace=None, out=None, lse=None):
+    """Causal attention of query tokens [L][N][heads][128] over 16-bit blocks [L][n][T][H][128] through tables [L][R][E] (int32).
+
+    ctx_len int32 [R]: cached tokens, this step's among them; q_start int32 [R+1]: a request's query tokens (None: one each);
+    max_q: most query tokens of a request, which chooses the kernel (None: as many as there are in all, which is always enough; a step that
+    knows that its requests have fewer says so, 1 when decoding).  Further tokens of a request are not computed: their rows, and those of tokens
+    that belong to no request, keep what out and lse held, or hold anything where these are new.
+    weights_out float32 [L][R][E] (a new one with want_weights or weights_in; may be weights_in): weights_in (None: nothing) and what the tokens of
+    every table entry gather of these queries' probabilities.
+    Returns dict(out [L][N][heads][128], lse float32 [L][N][heads] or None, weights float32 [L][R][E] or None)."""
+    shape, dtype = q.shape, q.dtype
+    d, blocks, L, N, heads, R, E, token, layer = _kv_attend_layout(shape, q.stride(), dtype, k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype,
+                                                                   tables.shape, tables.stride(), tables.dtype, ctx_len.shape, ctx_len.stride(),
+                                                                   ctx_len.dtype)
+    _dev(q, k, v, tables, ctx_len, q_start, weights_in, weights_out, workspace, out, lse)
+    if q_start is not None:
+        assert q_start.dtype == torch.int32 and q_start.shape == (R + 1,) and q_start.is_contiguous()
+    if max_q is None:
+        max_q = 1 if q_start is None else N
+    if weights_out is None and (want_weights or weights_in is not None):
+        weights_out = torch.empty((L, R, E), dtype=torch.float32, device=q.device)
+    for w in (weights_in, weights_out):
+        assert w is None or (w.shape == tables.shape and w.dtype == torch.float32 and w.is_contiguous()), "weights are float32 [L][R][E]"
+    if workspace is None:
+        need = lib().rc_kv_attend_workspace_size(d, blocks, R, E, heads, N, max_q, int(weights_out is not None))
+        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=q.device)
+    else:
+        assert workspace.is_contiguous(), "a workspace is contiguous"
+    if out is None:
+        out = torch.empty((L, N, heads, 128), dtype=dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((L, N, heads), dtype=torch.float32, device=q.device)
+    if lse is None:
+        _attend_out(shape, dtype, out.shape, out.stride(), out.dtype, None, None, None)
+    else:
+        _attend_out(shape, dtype, out.shape, out.stride(), out.dtype, lse.shape, lse.stride(), lse.dtype)
+    code = lib().rc_kv_attend(d, blocks, k.data_ptr(), v.data_ptr(), tables.data_ptr(), R, E, ctx_len.data_ptr(),
+                              None if q_start is None else q_start.data_ptr(), q.data_ptr(), N, heads, token, layer, max_q,
+                              128 ** -0.5 if scale is None else scale, window, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                              None if weights_in is None else weights_in.data_ptr(), None if weights_out is None else weights_out.data_ptr(),
+                              workspace.data_ptr(), workspace.nbytes, _stream())
+    if code:
+        _check(code)
+    return dict(out=out, lse=lse, weights=weights_out)
+
+
+def rc_kv_evict(tables, weights, ctx_len, keep, refcount, block_tokens, n_first=1, n_last=1, in_place=False, out=None):
+    """Table entries [L][R][E] beyond keep (int32 [R]) blocks a request leave, those of the smallest weights (float32 [L][R][E]) first; the first
+    n_first and last n_last used ones stay.  Returns dict(tables, refcount [L][NB], n_evicted int32 [L][R])."""
+    _dev(tables, weights, ctx_len, keep, refcount)
+    assert tables.dtype == torch.int32 and tables.dim() == 3 and tables.is_contiguous(), "tables are int32 [L][R][E]"
+    L, R, E = tables.shape
+    assert weights.dtype == torch.float32 and weights.shape == tables.shape and weights.is_contiguous(), "weights are float32 [L][R][E]"
+    for t in (ctx_len, keep):
+        assert t.dtype == torch.int32 and t.shape == (R,) and t.is_contiguous()
+    assert refcount.dtype == torch.int32 and refcount.dim() == 2 and refcount.shape[0] == L and refcount.is_contiguous(), "refcount is int32 [L][NB]"
+    if out is not None:
+        assert not in_place
+        t_out, r_out, n_evicted = out["tables"], out["refcount"], out["n_evicted"]
+        _dev(t_out, r_out, n_evicted)
+        assert t_out.dtype == torch.int32 and t_out.shape == tables.shape and t_out.is_contiguous()
+        assert r_out.dtype == torch.int32 and r_out.shape == refcount.shape and r_out.is_contiguous()
+        assert n_evicted.dtype == torch.int32 and n_evicted.shape == (L, R) and n_evicted.is_contiguous()
+    else:
+        t_out = tables if in_place else torch.empty_like(tables)
+        r_out = refcount if in_place else torch.empty_like(refcount)
+        n_evicted = torch.empty((L, R), dtype=torch.int32, device=tables.device)
+    _check(lib().rc_kv_evict(L, _ptr(tables), _ptr(t_out), R, E, refcount.shape[1], int(block_tokens), _ptr(ctx_len), _ptr(weights), _ptr(keep),
+                             int(n_first), int(n_last), _ptr(refcount), _ptr(r_out), _ptr(n_evicted), _stream()))
+    return dict(tables=t_out, refcount=r_out, n_evicted=n_evicted)

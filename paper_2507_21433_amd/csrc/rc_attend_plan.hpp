@@ -166,12 +166,13 @@ inline int64_t attend_most_units(const AttendShape& s) {
 constexpr int64_t kMostTokens = 0x7fffffffLL / 2;  // query tokens of a layer, and requests
 
 // The shape of a call; false where it is beyond what the kernels count in 32 bits.
+using AttendKernels = AttendKernel (*)(int64_t rows, double pairs, int64_t steps);
 inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_t T, int32_t H, int32_t n_heads, int64_t n_q, int64_t max_q,
-                         int64_t window) {
+                         int64_t window, AttendKernels kernels = attend_kernel) {
   const int32_t g = n_heads / H;
   if (max_q > n_q) max_q = n_q;
   if (E > (0x7fffffffLL - 64) / T || n_q > kMostTokens || R > kMostTokens || (max_q > 0 && max_q > 0x7fffff00LL / g)) return false;
-  const AttendKernel k = attend_kernel(max_q * g, (double)L * R * H, E * T / 64);
+  const AttendKernel k = kernels(max_q * g, (double)L * R * H, E * T / 64);
   // a window longer than any position is none
   *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.free, k.wgs,
         65536u / (uint32_t)g + 1, (int32_t)(L > 0 ? (kLongestLine - 1) / L : 0)};
@@ -206,7 +207,8 @@ inline size_t attend_workspace(const AttendShape& s) {
 }
 // The workspace of calls of up to max_q query tokens a request, however many there are in all: the largest of the kernels that fewer of them would take
 // as well.  Where so many requests of max_q tokens each are more than a call can have, calls of fewer tokens may have all workgroups.
-inline size_t attend_largest_workspace(int64_t L, int64_t R, int64_t E, int32_t T, int32_t H, int32_t n_heads, int64_t max_q) {
+inline size_t attend_largest_workspace(int64_t L, int64_t R, int64_t E, int32_t T, int32_t H, int32_t n_heads, int64_t max_q,
+                                       AttendKernels kernels = attend_kernel) {
   const int32_t g = n_heads / H;
   size_t most = 0;
   for (const int64_t rows : {(int64_t)16, (int64_t)32, (int64_t)64, max_q > kMostTokens ? kMostTokens * g : max_q * g}) {
@@ -214,10 +216,10 @@ inline size_t attend_largest_workspace(int64_t L, int64_t R, int64_t E, int32_t 
     if ((q < 1 && max_q > 0) || q > max_q) continue;
     AttendShape s;
     size_t n;
-    if (attend_shape(&s, L, R, E, T, H, n_heads, q && R > kMostTokens / q ? kMostTokens : R * q, q, 0)) {
+    if (attend_shape(&s, L, R, E, T, H, n_heads, q && R > kMostTokens / q ? kMostTokens : R * q, q, 0, kernels)) {
       n = attend_workspace(s);
     } else {
-      const AttendKernel k = attend_kernel(rows, 1e18, 1);
+      const AttendKernel k = kernels(rows, 1e18, 1);
       n = attend_header_bytes(k.wgs) + 2 * (size_t)k.wgs * attend_part_bytes(k.rows);
     }
     if (n > most) most = n;

@@ -15,19 +15,12 @@
 #include <hip/hip_runtime.h>
 
 #include "rc_common.hpp"
+#include "rc_vec.hpp"
 
 namespace rc {
 
 constexpr int kRecordBytes = 2176, kRecordV = 1024, kRecordKExp = 2048, kRecordVExp = 2112;
 constexpr int kNanByte = 255, kOneByte = 127;
-
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // The exponent byte b as the fp32 number that the conversions take: they use its exponent field, which makes 255 a NaN, and nothing
 // else of it (checked for all 256 exponents under any sign and fraction), so that byte `r` of a word takes one shift.

@@ -1,0 +1,902 @@
+// rc_kv_attend: softmax attention over 16-bit paged KV blocks, one pass over the data with a running reference of the softmax, and what
+// every block gathers of it.
+//
+// Scores are taken as S^T = K Q^T and outputs as O^T = V^T P^T on 16x16x32 matrix instructions: a row (a query token and head) is a
+// column of both, so that its scores, its probabilities and its sums lie in the same four lanes and the probabilities go from
+// one product into the next as they are.  A token's head is 256 bytes in a row of memory.  K's operand (a lane: 8 dims of a token) is what a
+// load of 16 bytes brings; V's (a lane: 8 tokens of a dim) are eight such loads, of eight tokens, whose halves are paired by one byte permute
+// for each two values: no value moves between lanes.
+#include <hip/hip_runtime.h>
+
+#include "rc_attend.hpp"
+#include "rc_kv.hpp"
+
+namespace rc {
+namespace {
+
+struct KvAttendArgs : AttendArgs {
+  const char *k, *v;
+  int64_t layer_stride_b;
+  uint32_t token_b, block_b;  // bytes of a token's heads, of a block
+  f32x4* gathered;            // few rows: what the rows' weights of a run of 32 tokens come to, [L][R][H][runs][rows]: of its two tiles, and their reference
+  int32_t runs, kept_rows;
+};
+
+// ---- Loads.
+
+// What a wave holds of 16 tokens: K in operand order (lane: token lane % 16, dims 32 d + 8 (lane / 16) on), V as it lies (lane: dims 8 (lane % 16) on of
+// tokens 4 (lane / 16) + r).
+struct KvTile {
+  u32x4 k[4], v[4];
+};
+struct KvLanes {
+  uint32_t k, v[4];  // the lane's offsets into a tile
+  __device__ __forceinline__ KvLanes(const KvAttendArgs& a, int lane) : k((lane & 15) * a.token_b + (lane >> 4) * 16) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = (4 * (lane >> 4) + r) * a.token_b + (lane & 15) * 16;
+  }
+};
+// STREAM: tokens that no other workgroup reads are not kept in the caches behind this one, where there are too many of them anyway.
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load16(const char* p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load((const u32x4*)p);
+  else
+    return *(const u32x4*)p;
+}
+template <bool STREAM>
+__device__ __forceinline__ void load_k(KvTile& x, const char* k, const KvLanes& at) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d) x.k[d] = load16<STREAM>(k + at.k + d * 64);
+}
+template <bool STREAM>
+__device__ __forceinline__ void load_v(KvTile& x, const char* v, const KvLanes& at) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) x.v[r] = load16<STREAM>(v + at.v[r]);
+}
+// Where the tile whose id lane j holds lies behind the layer's and head's first byte (its parity chooses between the halves of a block of 32); in block 0
+// where there is no such block (`there` false): its values are replaced or masked.
+__device__ __forceinline__ uint64_t tile_offset(const KvAttendArgs& a, int id, int parity, bool& there) {
+  there = id >= 0;
+  return (uint64_t)(uint32_t)(there ? id : 0) * a.block_b + (a.s.T == 32 ? parity * 16 * a.token_b : 0);
+}
+
+// Row n of q as lane (row, quarter) holds it for the four steps of K's dims; rows that the item does not have: its last one's.
+template <bool ONE>
+__device__ __forceinline__ void load_rows(const AttendArgs& a, const Walk& w, int n, int quarter, u32x4 (&q)[4]) {
+  n = min(n, w.q.rows - 1);
+  const int j = row_token<ONE>(a, n), head = w.h * a.s.g + n - j * a.s.g;
+  const char* p = a.q + (int64_t)w.l * a.q_layer_stride_b + (int64_t)(w.q.first + j) * a.q_token_stride_b + head * 256 + quarter * 16;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) q[s] = *(const u32x4*)(p + s * 64);
+}
+
+// V's operands of dims 8i + 2B and 8i + 2B + 1 (lane i of 16) from word B of four tokens: tokens 0 and 1 to one register, 2 and 3 to the next.
+template <int B>
+__device__ __forceinline__ void pair_v(const u32x4 (&v)[4], uint32_t (&even)[2], uint32_t (&odd)[2]) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    even[p] = __builtin_amdgcn_perm(v[2 * p + 1][B], v[2 * p][B], 0x05040100u);
+    odd[p] = __builtin_amdgcn_perm(v[2 * p + 1][B], v[2 * p][B], 0x07060302u);
+  }
+}
+
+// Whether any of a lane's values is a bf16 number of 2^65 or more (its exponent byte 192 or more).
+__device__ __forceinline__ uint32_t large_bits(const u32x4 (&v)[4]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m |= v[i >> 2][i & 3] & v[i >> 2][i & 3] << 1;
+  return m & 0x40004000u;
+}
+// Infinities and NaNs among two 16-bit values: their halves' bits.
+template <bool BF16>
+__device__ __forceinline__ uint32_t strange_half(uint32_t w) {
+  constexpr uint32_t inf = BF16 ? 0x7f80u : 0x7c00u;
+  return ((w & inf) == inf ? 0xffffu : 0u) | ((w >> 16 & inf) == inf ? 0xffff0000u : 0u);
+}
+// V of tokens that no row sees replaced by 0: whatever lies there (memory that was never written) gets a probability of 0, and 0 times infinity or NaN would
+// not be 0.  So are infinities and NaNs of tokens that only some rows may see: strange() adds them to these.  Token r of the lane stands at pos + r.  True if
+// there were such.
+template <bool BF16>
+__device__ inline bool seen_only(u32x4 (&v)[4], int pos, bool there, const AttendItem& it) {
+  const uint32_t span = there ? it.high_max - it.low_min : 0;  // (an item that sees no token has no run)
+  uint32_t found = 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const uint32_t keep = (uint32_t)(pos + r - it.low_min) < span ? ~0u : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = v[r][i] & keep, bad = strange_half<BF16>(x);
+      found |= bad;
+      v[r][i] = x & ~bad;
+    }
+  }
+  return found != 0;
+}
+// Infinities and NaNs of a tile's V (16 tokens from position pos on) into the sums of the rows that see them: the lane's row sees `span` positions from
+// low on.
+template <bool BF16>
+__device__ __forceinline__ void strange(f32x4 (&o)[8], const char* v, uint32_t token_b, int pos, int low, uint32_t span, int quarter) {
+#pragma unroll 1
+  for (int t = 0; t < 16; ++t) {
+    const bool seen = (uint32_t)(pos + t - low) < span;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const u32x4 x = *(const u32x4*)(v + t * token_b + (4 * quarter + r) * 16);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint32_t w = x[c >> 1], bad = strange_half<BF16>(w);
+        if (seen && (c & 1 ? bad >> 16 : bad & 0xffffu)) o[c][r] += c & 1 ? high16<BF16>(w) : low16<BF16>(w);
+      }
+    }
+  }
+}
+
+// ---- Few rows: every wave has all of an item's rows and every fourth run of 32 tokens.
+
+template <int RT>
+struct RowsLds {
+  float ref[kWaves][16 * RT], sum[kWaves][16 * RT];
+  float o[kWaves][16][132];
+};
+
+template <bool BF16, int RT, bool STREAM, bool WEIGH>
+__global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
+  // Probabilities as sums of two 16-bit numbers: with one row tile the matrix cores have the time, and the only rounding
+  // that counts is that of the output; with two tiles they are rounded once, which in the output is as much as its own rounding.
+  constexpr bool kTwo = RT == 1;
+  __shared__ RowsLds<RT> lds;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+  const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  const KvLanes lanes(a, lane);
+  Walk w;
+  if (!find<true>(a, wg, w)) return;
+  for (;;) {
+    Part part;
+    take_part<true>(a, w, part);
+    if (only_free(w, part)) {
+      leave_border(a, wg, -1, w);
+      return;
+    }
+    if (w.item.pairs == 0) {
+      store_nothing<true>(a, w);
+      if (!go_on<true>(a, wg, w, part)) return;
+      continue;
+    }
+    const int64_t head = (int64_t)w.l * a.layer_stride_b + w.h * 256;
+    const char *head_k = a.k + head, *head_v = a.v + head;
+    const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
+    f32x4* gathered = nullptr;
+    if constexpr (WEIGH) gathered = a.gathered + (((int64_t)w.l * a.s.R + w.r) * a.s.H + w.h) * (int64_t)a.runs * a.kept_rows;
+
+    // the wave's runs of 32 tokens: every fourth from pa + wave on
+    const int mine = (part.pb - part.pa - wave + kWaves - 1) / kWaves;
+    u32x4 q[RT][4];
+    f32x4 o[RT][8];
+    float ref[RT], sum[RT];
+    int low[RT];
+    uint32_t span[RT];  // of the positions that the lane's row sees, from low on
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      load_rows<true>(a, w, 16 * t + col, quarter, q[t]);
+      const int pos = row_position<true>(a, w, 16 * t + col);
+      low[t] = attend_low(a.s, pos), span[t] = max(attend_high(a.s, pos) - low[t], 0);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
+      ref[t] = kNothing, sum[t] = 0.f;
+    }
+
+    KvTile x[2];
+    uint64_t at[2] = {0, 0};
+    bool there[2], there_next[2] = {false, false};
+    Gate gate(a.c);
+    // Runs whose blocks are all gone are passed over: block ids of 32 runs at a time, a bit of `left` for each that has a block.
+    int ids = -1, batch = -32, n = 0;
+    uint64_t left = 0;
+    const auto next = [&]() -> bool {
+      while (left == 0) {
+        batch += 32;
+        if (batch >= mine) return false;
+        const int pair = part.pa + wave + kWaves * (batch + (lane >> 1));
+        ids = load_id(a, table, 2 * pair + (lane & 1), pair < part.pb);
+        const uint64_t b = __ballot(ids >= 0);
+        left = (b | b >> 1) & 0x5555555555555555ull;
+      }
+      const int bit = __builtin_ctzll(left);
+      left &= left - 1;
+      n = batch + (bit >> 1);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) at[j] = tile_offset(a, __builtin_amdgcn_readlane(ids, bit + j), j, there_next[j]);
+      return true;
+    };
+    bool more = next();
+    if (more) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_k<STREAM>(x[j], head_k + at[j], lanes);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], head_v + at[j], lanes);
+    }
+    // The next run's K is on its way from where this one's is used up, and V likewise.  The loads are never left out (behind the
+    // last run that one is loaded again): where a branch goes round them, a wait for some of the loads becomes a wait for all.
+#pragma unroll 1
+    while (more) {
+      const int pair = part.pa + wave + kWaves * n, pos = pair * kPairTokens;
+      const uint64_t here[2] = {at[0], at[1]};
+      there[0] = there_next[0], there[1] = there_next[1];
+      f32x4 s[RT][2];
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) s[t][j] = mfma<BF16>(x[j].k[d], q[t][d], d ? s[t][j] : f32x4{0, 0, 0, 0});
+      more = next();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_k<STREAM>(x[j], head_k + at[j], lanes);
+      // every row sees all 32 tokens, but at the ends of what the rows see and where the table has a hole
+      if (pos < w.item.low_max || pos + kPairTokens > w.item.high_min || !there[0] || !there[1]) {
+        bool odd[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) odd[j] = __any(seen_only<BF16>(x[j].v, pos + 16 * j + 4 * quarter, there[j], w.item));
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const bool is = (uint32_t)(pos + 16 * j + 4 * quarter + r - low[t]) < (there[j] ? span[t] : 0u);
+              s[t][j][r] = is ? s[t][j][r] : -__builtin_inff();
+            }
+            if (__builtin_expect(odd[j], 0)) strange<BF16>(o[t], head_v + here[j], a.token_b, pos + 16 * j, low[t], span[t], quarter);
+          }
+        }
+      }
+      if constexpr (BF16) {
+        if (__builtin_expect(__any((large_bits(x[0].v) | large_bits(x[1].v)) != 0), 0)) gate.see(true);
+      }
+      u32x4 hi[RT], lo[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float top = s[t][0][0];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
+        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, t, gate, lds.ref[wave][16 * t + col]);
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], gate.times[t], -ref[t]));
+        const float first = (p[0] + p[1]) + (p[2] + p[3]), second = (p[4] + p[5]) + (p[6] + p[7]);
+        sum[t] += first + second;
+        if constexpr (WEIGH) {
+          const float a0 = row_sum(first), a1 = row_sum(second);
+          if (quarter == 0 && 16 * t + col < w.q.rows)
+            gathered[(int64_t)pair * a.kept_rows + 16 * t + col] = f32x4{a0, a1, gate.odd >> t & 1 ? lds.ref[wave][16 * t + col] : ref[t], 0};
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t two = kTwo ? cut2<BF16>(p[2 * j], p[2 * j + 1]) : pack2<BF16>(p[2 * j], p[2 * j + 1]);
+          hi[t][j] = two;
+          if (kTwo) lo[t][j] = cut2<BF16>(p[2 * j] - low16<BF16>(two), p[2 * j + 1] - high16<BF16>(two));
+        }
+      }
+      const auto chunks = [&](auto b) {
+        constexpr int B = decltype(b)::value;
+        uint32_t e0[2], d0[2], e1[2], d1[2];
+        pair_v<B>(x[0].v, e0, d0);
+        pair_v<B>(x[1].v, e1, d1);
+        const u32x4 even = {e0[0], e0[1], e1[0], e1[1]}, odd = {d0[0], d0[1], d1[0], d1[1]};
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          o[t][2 * B] = mfma<BF16>(even, hi[t], o[t][2 * B]);
+          o[t][2 * B + 1] = mfma<BF16>(odd, hi[t], o[t][2 * B + 1]);
+          if (kTwo) {
+            o[t][2 * B] = mfma<BF16>(even, lo[t], o[t][2 * B]);
+            o[t][2 * B + 1] = mfma<BF16>(odd, lo[t], o[t][2 * B + 1]);
+          }
+        }
+      };
+      chunks(std::integral_constant<int, 0>{});
+      chunks(std::integral_constant<int, 1>{});
+      chunks(std::integral_constant<int, 2>{});
+      chunks(std::integral_constant<int, 3>{});
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], head_v + at[j], lanes);
+    }
+
+    // the four waves' sums, under the largest of their references
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      sum[t] = row_sum(sum[t]);
+      if (gate.odd >> t & 1) ref[t] = lds.ref[wave][16 * t + col];
+      if (quarter == 0) lds.ref[wave][16 * t + col] = ref[t], lds.sum[wave][16 * t + col] = sum[t];
+    }
+    __syncthreads();
+    float* to_part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(16 * RT));
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      float top = kNothing;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) top = fmaxf(top, lds.ref[v][16 * t + col]);
+      const float f = __builtin_amdgcn_exp2f(ref[t] - top);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float* to = &lds.o[wave][col][(4 * quarter + r) * 8];
+        *(f32x4*)to = f32x4{o[t][0][r], o[t][1][r], o[t][2][r], o[t][3][r]} * f;
+        *(f32x4*)(to + 4) = f32x4{o[t][4][r], o[t][5][r], o[t][6][r], o[t][7][r]} * f;
+      }
+      __syncthreads();
+      // a thread adds eight dims of a row
+      const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8, m = 16 * t + row;
+      if (m < w.q.rows) {
+        float most = kNothing, all = 0.f;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) most = fmaxf(most, lds.ref[v][m]);
+        f32x4 y0 = {0, 0, 0, 0}, y1 = {0, 0, 0, 0};
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) {
+          all += lds.sum[v][m] * __builtin_amdgcn_exp2f(lds.ref[v][m] - most);
+          y0 += *(const f32x4*)&lds.o[v][row][d];
+          y1 += *(const f32x4*)&lds.o[v][row][d + 4];
+        }
+        if (part.whole) {
+          const float f1 = row_scale(all);
+          const int64_t place = row_place<true>(a, w, m);
+          y0 *= f1, y1 *= f1;
+          *(u32x4*)(a.out + (place * 128 + d) * 2) = u32x4{pack2<BF16>(y0[0], y0[1]), pack2<BF16>(y0[2], y0[3]), pack2<BF16>(y1[0], y1[1]), pack2<BF16>(y1[2], y1[3])};
+          if (d == 0 && a.lse) a.lse[place] = row_lse(most, all);
+          if (WEIGH && d == 0) a.ends[place] = float2{most, all};
+        } else {
+          *(f32x4*)(to_part + m * 128 + d) = y0;
+          *(f32x4*)(to_part + m * 128 + d + 4) = y1;
+          if (d == 0) *(float2*)(to_part + 16 * RT * 128 + m * 2) = float2{most, all};
+        }
+      }
+      __syncthreads();
+    }
+    if (!go_on<true>(a, wg, w, part)) return;
+  }
+}
+
+// ---- Many rows: every wave has 32 of an item's 128 rows (16 of 64 with one row tile), and the workgroup lays 64 tokens at a time out as operands
+// in LDS, once for all of its rows: every wave 16 tokens, into the buffer that the step does not read.
+
+struct ManyLds {
+  u32x4 k[2][4][4][64];     // [buffer][16 tokens][step of the dims][lane]
+  u32x2 v[2][2][8][64][2];  // [buffer][32 tokens][chunk][lane][16 tokens of the 32]
+  int32_t there[2][4];      // of the tiles of a buffer: whether there is a block (1), large V (16), infinities or NaNs that only some rows may see (32)
+  float ref[kWaves][32];    // references of odd row tiles
+};
+
+template <bool BF16, int RT>
+__global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(KvAttendArgs a) {
+  constexpr int kStep = 64, kRows = kWaves * 16 * RT;
+  __shared__ ManyLds lds;
+  const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
+  const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  const KvLanes lanes(a, lane);
+  Walk w;
+  if (!find<false>(a, wg, w)) return;
+  for (;;) {
+    Part cut;
+    if (!take_part<false>(a, w, cut)) continue;
+    if (only_free(w, cut)) {
+      leave_border(a, wg, -1, w);
+      return;
+    }
+    if (w.item.pairs == 0) {
+      store_nothing<false>(a, w);
+      if (!go_on<false>(a, wg, w, cut)) return;
+      continue;
+    }
+    const int pa = cut.pa, pb = cut.pb;
+    const int64_t head = (int64_t)w.l * a.layer_stride_b + w.h * 256;
+    const char *head_k = a.k + head, *head_v = a.v + head;
+    const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
+    const int steps = (pb - pa + 1) / 2, row0 = w.t * kRows + wave * 16 * RT;
+    const bool busy = row0 < w.q.rows;
+
+    u32x4 q[RT][4];
+    f32x4 o[RT][8];
+    float ref[RT], sum[RT];
+    int low[RT];
+    uint32_t span[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int n = row0 + 16 * t + col;
+      load_rows<false>(a, w, n, quarter, q[t]);
+      const int pos = row_position<false>(a, w, n);
+      low[t] = attend_low(a.s, pos), span[t] = max(attend_high(a.s, pos) - low[t], 0);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
+      ref[t] = kNothing, sum[t] = 0.f;
+    }
+
+    const auto at_ends = [&](int pos) { return pos < w.item.low_max || pos + kStep > w.item.high_min; };
+    Gate gate(a.c);
+    // the wave's 16 tokens of a step
+    int ids = -1;
+    const auto load = [&](KvTile& x, bool& there, int step) {
+      if ((step & 63) == 0) {
+        const int pair = pa + 2 * (step + lane) + (wave >> 1);
+        ids = load_id(a, table, 2 * pair + (wave & 1), pair < pb);
+      }
+      const uint64_t at = tile_offset(a, __builtin_amdgcn_readlane(ids, step & 63), wave & 1, there);
+      load_k<false>(x, head_k + at, lanes);
+      load_v<false>(x, head_v + at, lanes);
+    };
+    const auto lay = [&](KvTile& x, bool there, int step, int buf) {
+      const int pos = (pa + 2 * step) * kPairTokens;
+      int flags = there;
+      if (at_ends(pos) || !there) flags |= __any(seen_only<BF16>(x.v, pos + 16 * wave + 4 * quarter, there, w.item)) ? 32 : 0;
+      if constexpr (BF16) flags |= __any(large_bits(x.v) != 0) ? 16 : 0;
+      if (lane == 0) lds.there[buf][wave] = flags;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) lds.k[buf][wave][d][lane] = x.k[d];
+      const auto chunks = [&](auto b) {
+        constexpr int B = decltype(b)::value;
+        uint32_t e[2], d[2];
+        pair_v<B>(x.v, e, d);
+        lds.v[buf][wave >> 1][2 * B][lane][wave & 1] = u32x2{e[0], e[1]};
+        lds.v[buf][wave >> 1][2 * B + 1][lane][wave & 1] = u32x2{d[0], d[1]};
+      };
+      chunks(std::integral_constant<int, 0>{});
+      chunks(std::integral_constant<int, 1>{});
+      chunks(std::integral_constant<int, 2>{});
+      chunks(std::integral_constant<int, 3>{});
+    };
+    const auto attend = [&](int step, int buf) {
+      const int pos = (pa + 2 * step) * kPairTokens;
+      // Operands come from LDS four at a time, while the products of the four before them run: left to the compiler, every read is
+      // waited for by itself.
+      f32x4 s[RT][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0, 0, 0, 0};
+      u32x4 k[2][4];
+      const auto read_k = [&](int i) {  // tiles 2 (i / 2) and the next, steps 2 (i % 2) and the next
+#pragma unroll
+        for (int m = 0; m < 4; ++m) k[i & 1][m] = lds.k[buf][(i & 2) + (m & 1)][2 * (i & 1) + (m >> 1)][lane];
+      };
+      read_k(0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i < 3) read_k(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) s[t][(i & 2) + (m & 1)] = mfma<BF16>(k[i & 1][m], q[t][2 * (i & 1) + (m >> 1)], s[t][(i & 2) + (m & 1)]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      int f[4], all = 15, any = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = uniform(lds.there[buf][j]), any |= f[j], all &= f[j];
+      if constexpr (BF16) gate.see((any & 16) != 0);
+      if (at_ends(pos) || !(all & 1)) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const bool is = (uint32_t)(pos + 16 * j + 4 * quarter + r - low[t]) < (f[j] & 1 ? span[t] : 0u);
+              s[t][j][r] = is ? s[t][j][r] : -__builtin_inff();
+            }
+        }
+        if (__builtin_expect(any & 32, 0)) {
+#pragma unroll 1
+          for (int j = 0; j < 4; ++j) {
+            if (!(uniform(lds.there[buf][j]) & 32)) continue;
+            bool there;
+            const int tile = 2 * (pa + 2 * step) + j;
+            const uint64_t at = tile_offset(a, uniform(load_id(a, table, tile, true)), tile & 1, there);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) strange<BF16>(o[t], head_v + at, a.token_b, pos + 16 * j, low[t], span[t], quarter);
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float top = s[t][0][0];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
+        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, t, gate, lds.ref[wave][16 * t + col]);
+      }
+      u32x4 v[8], p16[RT][2];
+      const auto read_v = [&](int i) {  // the chunks of tokens 32 i and the next
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = *(const u32x4*)&lds.v[buf][i][c][lane][0];
+      };
+      const auto weigh = [&](int i) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          float p[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + (j >> 2)][j & 3], gate.times[t], -ref[t]));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p16[t][i][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
+          sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        }
+      };
+      const auto add = [&](int i) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) o[t][c] = mfma<BF16>(v[c], p16[t][i], o[t][c]);
+      };
+      read_v(0);
+      weigh(0);
+      add(0);
+      weigh(1);
+      read_v(1);
+      add(1);
+    };
+
+    KvTile x;
+    bool there;
+    if (steps > 0) {
+      load(x, there, 0);
+      lay(x, there, 0, 0);
+    }
+    __syncthreads();
+    // behind the last step a tile of no block is loaded and laid into the buffer that is free
+    for (int step = 0; step < steps; ++step) {
+      load(x, there, step + 1);
+      if (busy) attend(step, step & 1);
+      lay(x, there, step + 1, ~step & 1);
+      __syncthreads();
+    }
+
+    float* part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(kRows));
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float all = row_sum(sum[t]);
+      if (gate.odd >> t & 1) ref[t] = lds.ref[wave][16 * t + col];
+      const int m = wave * 16 * RT + 16 * t + col, n = w.t * kRows + m;
+      if (n >= w.q.rows) continue;
+      if (cut.whole) {
+        const float f = row_scale(all);
+        const int64_t place = row_place<false>(a, w, n);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *(u32x4*)(a.out + (place * 128 + (4 * quarter + r) * 8) * 2) =
+              u32x4{pack2<BF16>(o[t][0][r] * f, o[t][1][r] * f), pack2<BF16>(o[t][2][r] * f, o[t][3][r] * f),
+                    pack2<BF16>(o[t][4][r] * f, o[t][5][r] * f), pack2<BF16>(o[t][6][r] * f, o[t][7][r] * f)};
+        if (quarter == 0 && a.lse) a.lse[place] = row_lse(ref[t], all);
+        if (quarter == 0 && a.ends) a.ends[place] = float2{ref[t], all};
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          *(f32x4*)(part + m * 128 + (4 * quarter + r) * 8) = f32x4{o[t][0][r], o[t][1][r], o[t][2][r], o[t][3][r]};
+          *(f32x4*)(part + m * 128 + (4 * quarter + r) * 8 + 4) = f32x4{o[t][4][r], o[t][5][r], o[t][6][r], o[t][7][r]};
+        }
+        if (quarter == 0) part[kRows * 128 + m * 2] = ref[t], part[kRows * 128 + m * 2 + 1] = all;
+      }
+    }
+    if (!go_on<false>(a, wg, w, cut)) return;
+  }
+}
+
+// ---- What blocks gather.
+
+struct WeighArgs {
+  KvAttendArgs a;
+  const float* in;
+  float* out;
+  float* sums;  // many rows: of the rows of a share and KV head, [share][L][R][H][tiles of 16 tokens]
+  int32_t tiles, shares;
+};
+
+// Many rows: the probabilities are taken once more, from K, Q and the rows' final references and sums: a wave holds the K of 128 tokens and goes through a
+// share of the request's rows.  (Kept from the first time they would be a number for each row and 16 tokens: 10 GB for a prompt of 32k tokens and 40 heads.)
+constexpr int kWeighTiles = 8;
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
+  const KvAttendArgs& a = g.a;
+  const int lane = threadIdx.x & 63, quarter = lane >> 4, col = lane & 15, chunks = (g.tiles + kWeighTiles - 1) / kWeighTiles;
+  const int64_t tasks = a.s.L * a.s.R * a.s.H * chunks * (int64_t)g.shares;
+  for (int64_t task = (int64_t)blockIdx.x * kWaves + uniform((int)(threadIdx.x >> 6)); task < tasks; task += (int64_t)gridDim.x * kWaves) {
+    // shares beside each other: they read the same K
+    int64_t i = task / g.shares;
+    const int share = (int)(task - i * g.shares), chunk = (int)(i % chunks);
+    i /= chunks;
+    Walk w;
+    w.h = (int)(i % a.s.H);
+    i /= a.s.H;
+    w.r = (int)(i % a.s.R), w.l = (int)(i / a.s.R), w.t = 0;
+    w.q = request(a, w.r);
+    const int pos0 = chunk * kWeighTiles * 16, first = w.q.ctx - w.q.len;
+    if (w.q.rows == 0) continue;
+    // the rows that see any of these tokens
+    const int last = first + (w.q.rows - 1) / a.s.g;
+    if (attend_high(a.s, last) <= pos0 || attend_low(a.s, first) >= pos0 + kWeighTiles * 16) continue;
+    const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
+    const char* head_k = a.k + (int64_t)w.l * a.layer_stride_b + w.h * 256 + (lane & 15) * a.token_b + quarter * 16;
+    u32x4 k[kWeighTiles][4];
+    int there = 0;
+    const int ids = load_id(a, table, chunk * kWeighTiles + (lane & 7), true);
+#pragma unroll
+    for (int j = 0; j < kWeighTiles; ++j) {
+      bool is;
+      const uint64_t at = tile_offset(a, __builtin_amdgcn_readlane(ids, j), j & 1, is);
+      there |= (int)is << j;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) k[j][d] = *(const u32x4*)(head_k + at + d * 64);
+    }
+    float sum[kWeighTiles];
+#pragma unroll
+    for (int j = 0; j < kWeighTiles; ++j) sum[j] = 0.f;
+    const int row_tiles = (w.q.rows + 15) / 16, from = (int)((int64_t)row_tiles * share / g.shares), to = (int)((int64_t)row_tiles * (share + 1) / g.shares);
+#pragma unroll 1
+    for (int t = from; t < to; ++t) {
+      const int n = t * 16 + col, n_last = min(t * 16 + 15, w.q.rows - 1);
+      const int p0 = first + t * 16 / a.s.g, p1 = first + n_last / a.s.g;
+      if (attend_high(a.s, p1) <= pos0 || attend_low(a.s, p0) >= pos0 + kWeighTiles * 16) continue;
+      u32x4 q[4];
+      load_rows<false>(a, w, n, quarter, q);
+      float2 end = {0.f, 0.f};
+      if (n < w.q.rows) end = a.ends[row_place<false>(a, w, n)];
+      const float f = row_scale(end.y);
+      const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) < pos0 + kWeighTiles * 16 || there != 255;
+      const int pos = first + min(n, w.q.rows - 1) / a.s.g, low = attend_low(a.s, pos);
+      const uint32_t span = max(attend_high(a.s, pos) - low, 0);
+      const bool coarse = uniform(__any(f != 0.f && fabsf(end.x) > kCoarse));
+#pragma unroll
+      for (int j = 0; j < kWeighTiles; ++j) {
+        f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+        for (int d = 0; d < 4; ++d) s = mfma<BF16>(k[j][d], q[d], s);
+        if (ends) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool is = (uint32_t)(pos0 + 16 * j + 4 * quarter + r - low) < (there >> j & 1 ? span : 0u);
+            s[r] = is ? s[r] : -__builtin_inff();
+          }
+        }
+        float p[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float e = fmaf(s[r], a.c, -end.x);
+          if (coarse) {
+#pragma clang fp contract(off)
+            const float z = s[r] * a.c, d = z - end.x;
+            e = fabsf(end.x) > kCoarse ? d : e;
+          }
+          p[r] = __builtin_amdgcn_exp2f(e);
+        }
+        // a row that sees nothing has no weights (f is 0, and what it would be multiplied with need not be a number)
+        const float add = ((p[0] + p[1]) + (p[2] + p[3])) * f;
+        sum[j] += f == 0.f ? 0.f : add;
+      }
+    }
+    float* sums = g.sums + ((((int64_t)share * a.s.L + w.l) * a.s.R + w.r) * a.s.H + w.h) * (int64_t)g.tiles + chunk * kWeighTiles;
+#pragma unroll
+    for (int j = 0; j < kWeighTiles; ++j) {
+      float x = row_sum(sum[j]);
+#pragma unroll
+      for (int d = 8; d; d >>= 1) x += __shfl_xor(x, d);
+      if (lane == 0 && chunk * kWeighTiles + j < g.tiles) sums[j] = x;
+    }
+  }
+}
+
+// Eight lanes add up what the rows of an entry's KV heads left, every lane of every eighth of them.
+template <bool FEW>
+__global__ __launch_bounds__(kThreads) void weigh_entries_kernel(WeighArgs g) {
+  const KvAttendArgs& a = g.a;
+  const int64_t E = a.s.E, at = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3), total = a.s.L * a.s.R * E;
+  const int part = threadIdx.x & 7;
+  if (at >= total) return;
+  const int e = (int)(at % E);
+  const int64_t lr = at / E;
+  const int r = (int)(lr % a.s.R), l = (int)(lr / a.s.R);
+  const AttendRequest q = request(a, r);
+  float sum = 0.f;
+  if (q.rows) {
+    const int first = q.ctx - q.len, last = first + (q.rows - 1) / a.s.g;
+    const int low = attend_low(a.s, first), high = attend_high(a.s, last);
+    const int id = a.tables[at];
+    const int64_t begin = (int64_t)e * a.s.T;
+    if (id >= 0 && id < a.n_blocks && begin < high && begin + a.s.T > low) {
+      const int per = a.s.T >> 4;
+      if constexpr (FEW) {
+        const int pair = per == 2 ? e : e >> 1;
+        const f32x4* gathered = a.gathered + (lr * a.s.H * (int64_t)a.runs + pair) * a.kept_rows;
+        for (int i = part; i < a.s.H * q.rows; i += 8) {
+          const int h = i / q.rows, n = i - h * q.rows;
+          const f32x4 x = gathered[(int64_t)h * a.runs * a.kept_rows + n];
+          const float2 end = a.ends[row_place<false>(a, l, h, q.first, n)];
+          const float w = per == 2 ? x[0] + x[1] : e & 1 ? x[1] : x[0];
+          const float p = w * __builtin_amdgcn_exp2f(x[2] - end.x) * row_scale(end.y);
+          sum += end.y == 0.f ? 0.f : p;
+        }
+      } else {
+        const float* sums = g.sums + lr * a.s.H * (int64_t)g.tiles + (int64_t)e * per;
+        const int64_t step = a.s.L * a.s.R * a.s.H * (int64_t)g.tiles;
+        for (int i = part; i < a.s.H * g.shares; i += 8) {
+          const int share = i / a.s.H, h = i - share * a.s.H;
+          const float* x = sums + share * step + (int64_t)h * g.tiles;
+          sum += per == 2 ? x[0] + x[1] : x[0];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 4; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if (part == 0) g.out[at] = g.in ? g.in[at] + sum : sum;
+}
+
+// ---- The call.
+
+// What the workspace holds behind the parts of cut items, where blocks are weighed.
+struct WeighRoom {
+  int64_t ends, gathered, sums;  // bytes
+  int32_t shares;
+  int64_t bytes() const { return ends + gathered + sums; }
+};
+constexpr int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+constexpr int kFewRows = 32, kMostShares = 16;
+constexpr int64_t kMostEntries = 1 << 29;  // table entries of a call that weighs them
+
+inline int64_t runs_of(const AttendShape& s) { return ((int64_t)s.cap + 31) / 32; }
+inline WeighRoom few_room(int64_t L, int64_t R, int64_t H, int64_t runs, int64_t rows) { return {0, L * R * H * runs * rows * 16, 0, 0}; }
+inline WeighRoom many_room(int64_t L, int64_t R, int64_t H, int64_t runs, int64_t rows) {
+  // a few thousand waves, of 8 row tiles at least
+  const double chunks = (double)L * R * H * ((runs * 2 + kWeighTiles - 1) / kWeighTiles);
+  int64_t shares = 1;
+  while (shares < kMostShares && shares * 2 * 128 <= rows && chunks * shares < 4096) shares *= 2;
+  return {0, 0, up16(shares * L * R * H * runs * 2 * 4), (int32_t)shares};
+}
+inline WeighRoom weigh_room(const AttendShape& s) {
+  const int64_t rows = (int64_t)s.max_q * s.g, runs = runs_of(s);
+  WeighRoom r = rows <= kFewRows ? few_room(s.L, s.R, s.H, runs, rows) : many_room(s.L, s.R, s.H, runs, rows);
+  r.ends = up16(s.L * s.n_q * s.H * s.g * 8);
+  return r;
+}
+
+rc_status kv_check(const rc_kv_desc* d, int64_t n_blocks, int64_t R, int64_t E, int32_t n_heads, int64_t n_q, int64_t max_q, int64_t window, bool weigh,
+                   AttendShape* s, const char* who) {
+  if (rc_status e = check_paged(d, n_blocks, who)) return e;
+  if (R < 0 || E < 0 || n_q < 0 || max_q < 0 || window < 0) return fail(RC_ERR_INVALID_ARG, "%s: negative size", who);
+  if (n_heads < 1 || n_heads % d->n_kv_heads != 0)
+    return fail(RC_ERR_INVALID_ARG, "%s: n_heads %d is not a multiple of n_kv_heads %d", who, n_heads, d->n_kv_heads);
+  if (n_heads > 1024) return fail(RC_ERR_UNSUPPORTED, "%s: n_heads %d (at most 1024)", who, n_heads);
+  if (!attend_shape(s, d->n_layers, R, n_blocks ? E : 0, d->block_tokens, d->n_kv_heads, n_heads, n_q, max_q, window))
+    return fail(RC_ERR_UNSUPPORTED, "%s: a table of 2^31 positions or more, or more than 2^30 query tokens, requests or row tiles", who);
+  if (weigh && (double)d->n_layers * R * E > (double)kMostEntries) return fail(RC_ERR_UNSUPPORTED, "%s: more than 2^29 table entries to weigh", who);
+  return RC_OK;
+}
+
+// Whether a call's tables can hold more than the last-level cache keeps from one pass over them to the next.
+inline bool kv_streams(const AttendShape& s) {
+  const double seen = s.window && (double)s.window + s.max_q < s.cap ? (double)s.window + s.max_q : s.cap;
+  return (double)s.L * s.R * s.H * seen * 512 > 384e6;
+}
+
+template <bool BF16, bool STREAM, bool WEIGH>
+void kv_rows_launch(const KvAttendArgs& a, hipStream_t st) {
+  if (a.s.rows == 16)
+    kv_rows_kernel<BF16, 1, STREAM, WEIGH><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
+  else
+    kv_rows_kernel<BF16, 2, STREAM, WEIGH><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
+}
+
+template <bool BF16>
+void kv_launch(const WeighArgs& g, hipStream_t st) {
+  const KvAttendArgs& a = g.a;
+  const bool stream = kv_streams(a.s), few = a.s.rows <= kFewRows;
+  if (few && g.out)
+    stream ? kv_rows_launch<BF16, true, true>(a, st) : kv_rows_launch<BF16, false, true>(a, st);
+  else if (few)
+    stream ? kv_rows_launch<BF16, true, false>(a, st) : kv_rows_launch<BF16, false, false>(a, st);
+  else if (a.s.rows == 64)
+    kv_many_kernel<BF16, 1><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
+  else
+    kv_many_kernel<BF16, 2><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
+  if (a.borders) {
+    const int64_t rows = (int64_t)a.s.max_q * a.s.g;
+    if (few)
+      attend_join_kernel<BF16, true><<<dim3(a.s.wgs - 1, (unsigned)(rows < a.s.rows ? rows : a.s.rows)), kThreads, 0, st>>>(a);
+    else
+      attend_join_kernel<BF16, false><<<dim3(a.s.wgs - 1, 8), kThreads, 0, st>>>(a);
+  }
+  if (!g.out) return;
+  const int64_t entries = a.s.L * a.s.R * a.s.E;
+  if (!few) {
+    const int64_t tasks = a.s.L * a.s.R * a.s.H * ((g.tiles + kWeighTiles - 1) / kWeighTiles) * (int64_t)g.shares, wgs = (tasks + kWaves - 1) / kWaves;
+    weigh_many_kernel<BF16><<<dim3((unsigned)(wgs < (1 << 22) ? wgs : (1 << 22))), kThreads, 0, st>>>(g);
+  }
+  const dim3 grid((unsigned)((entries + 31) / 32));
+  few ? weigh_entries_kernel<true><<<grid, kThreads, 0, st>>>(g) : weigh_entries_kernel<false><<<grid, kThreads, 0, st>>>(g);
+}
+
+// Nothing was asked: what was gathered before is what there is.
+__global__ __launch_bounds__(kThreads) void weigh_nothing_kernel(const float* in, float* out, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) out[i] = in ? in[i] : 0.f;
+}
+
+}  // namespace
+}  // namespace rc
+
+extern "C" size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_blocks, int64_t R, int64_t E, int32_t n_heads, int64_t n_q, int64_t max_q,
+                                              int32_t weigh) {
+  using namespace rc;
+  clear_error();
+  AttendShape s;
+  const int64_t q = max_q < 1 ? max_q : 1;
+  if (n_q < 0) return 0;
+  if (kv_check(desc, n_blocks, R, E, n_heads, q, q, 0, weigh != 0, &s, "rc_kv_attend_workspace_size")) return 0;
+  size_t n = attend_largest_workspace(s.L, R, s.E, s.T, s.H, n_heads, max_q);
+  if (weigh && max_q > 0) {
+    if ((double)s.L * n_q * n_heads > 1e15) return 0;
+    const int64_t runs = runs_of(s), few = max_q < kFewRows / s.g ? max_q : kFewRows / s.g;
+    const int64_t a = few_room(s.L, R, s.H, runs, few * s.g).bytes(), b = kMostShares * many_room(s.L, R, s.H, runs, 1).bytes();
+    n = (size_t)up16((int64_t)n) + (size_t)up16(s.L * n_q * n_heads * 8) + (size_t)(max_q * s.g > kFewRows && b > a ? b : a);
+  }
+  return n;
+}
+
+extern "C" rc_status rc_kv_attend(const rc_kv_desc* desc, int64_t n_blocks, const void* k, const void* v, const int32_t* tables, int64_t R, int64_t E,
+                                  const int32_t* ctx_len, const int32_t* q_start, const void* q, int64_t n_q, int32_t n_heads, int64_t q_token_stride,
+                                  int64_t q_layer_stride, int64_t max_q, float scale, int64_t window, void* out, float* lse, const float* weights_in,
+                                  float* weights_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  using namespace rc;
+  const char* who = "rc_kv_attend";
+  clear_error();
+  WeighArgs g;
+  KvAttendArgs& a = g.a;
+  if (rc_status e = kv_check(desc, n_blocks, R, E, n_heads, n_q, max_q, window, weights_out != nullptr, &a.s, who)) return e;
+  if (!q_start && (max_q > 1 || n_q < R)) return fail(RC_ERR_INVALID_ARG, "%s: without q_start there is one query token per request", who);
+  a.c = scale * 1.4426950408889634f;
+  if (!(scale > 0.f) || !(a.c < __builtin_inff()))
+    return fail(RC_ERR_INVALID_ARG, "%s: scale must be positive, and scale * log2(e) an fp32 number", who);
+  if (weights_in && !weights_out) return fail(RC_ERR_INVALID_ARG, "%s: weights_in without weights_out", who);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const int64_t entries = weights_out ? (int64_t)desc->n_layers * R * E : 0;
+  const auto keep_weights = [&] {
+    if (entries == 0 || weights_in == weights_out) return RC_OK;
+    weigh_nothing_kernel<<<dim3((unsigned)((entries + kThreads - 1) / kThreads)), kThreads, 0, st>>>(weights_in, weights_out, entries);
+    return check_launch(who);
+  };
+  if (desc->n_layers == 0 || R == 0 || n_q == 0 || max_q == 0) return keep_weights();
+  const bool empty = a.s.cap == 0;  // nothing to see: no table and no blocks are read
+  if (!ctx_len || !q || !out || (!empty && (!k || !v || !tables))) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
+  if (!aligned16(q) || !aligned16(out) || (!empty && (!aligned16(k) || !aligned16(v)))) return fail(RC_ERR_INVALID_ARG, "%s: pointer not 16-byte aligned", who);
+  if (q_token_stride < (int64_t)n_heads * 128 || q_token_stride > INT64_MAX / 4 / n_q || q_token_stride % 8 != 0 || q_layer_stride % 8 != 0)
+    return fail(RC_ERR_INVALID_ARG, "%s: q_token_stride smaller than n_heads*Dh, or a stride that breaks 16-byte alignment", who);
+  if (desc->n_layers > 1 && q_layer_stride < (int64_t)n_heads * 128) return fail(RC_ERR_INVALID_ARG, "%s: q_layer_stride smaller than a token", who);
+  const size_t parts = attend_workspace(a.s);
+  WeighRoom room = {0, 0, 0, 0};
+  if (weights_out) {
+    if ((double)a.s.L * n_q * n_heads > 1e15) return fail(RC_ERR_UNSUPPORTED, "%s: too many rows to weigh", who);
+    room = weigh_room(a.s);
+  }
+  const size_t need = parts && weights_out ? (size_t)up16((int64_t)parts) + (size_t)room.bytes() : parts + (size_t)room.bytes();
+  if (need) {
+    if (!workspace || workspace_bytes < need) return fail(RC_ERR_WORKSPACE, "%s: needs %zu bytes of workspace", who, need);
+    if (!aligned16(workspace)) return fail(RC_ERR_WORKSPACE, "%s: workspace not 16-byte aligned", who);
+  }
+  a.k = (const char*)k, a.v = (const char*)v, a.tables = tables, a.ctx_len = ctx_len, a.q_start = q_start;
+  a.q = (const char*)q, a.out = (char*)out, a.lse = lse;
+  a.layer_stride_b = desc->layer_stride * 2, a.q_token_stride_b = q_token_stride * 2, a.q_layer_stride_b = q_layer_stride * 2;
+  a.token_b = (uint32_t)desc->n_kv_heads * 256, a.block_b = a.token_b * (uint32_t)desc->block_tokens;
+  a.n_blocks = n_blocks;
+  a.borders = parts ? (AttendBorder*)workspace : nullptr;
+  a.parts = parts ? (char*)workspace + attend_header_bytes(a.s.wgs) : nullptr;
+  char* at = (char*)workspace + up16((int64_t)parts);
+  a.ends = weights_out ? (float2*)at : nullptr;
+  a.gathered = (f32x4*)(at + room.ends);
+  a.runs = (int32_t)runs_of(a.s), a.kept_rows = (int32_t)a.s.max_q * a.s.g;
+  g.sums = (float*)(at + room.ends + room.gathered);
+  g.in = weights_in, g.out = empty ? nullptr : weights_out, g.tiles = a.runs * 2, g.shares = room.shares;
+  if (desc->dtype == RC_BF16)
+    kv_launch<true>(g, st);
+  else
+    kv_launch<false>(g, st);
+  if (rc_status e = check_launch(who)) return e;
+  return empty ? keep_weights() : RC_OK;
+}

@@ -110,13 +110,28 @@ __device__ __forceinline__ void leave_border(const AttendArgs& a, int wg, int la
   if (a.borders && threadIdx.x == 0) a.borders[wg] = {last, w.at == w.begin, w.l, w.h, w.t * a.s.rows, w.q.rows, w.q.first, 0};
 }
 
-// ONE: a request has one row tile at most.
+// Sums over `lanes` neighbouring lanes, a power of two.
+__device__ __forceinline__ int add_lanes(int x, int lanes) {
+#pragma unroll 1
+  for (int d = 1; d < lanes; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ int upto_lane(int x, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x = attend_sum(x, y);
+  }
+  return x;
+}
+// Units of a request and KV head, counted by `lanes` lanes of which this one is number i.  ONE: a request has one row tile at most (and one lane counts it).
 template <bool ONE>
-__device__ __forceinline__ int units_of(const AttendArgs& a, const AttendRequest& q) {
-  if constexpr (ONE)
-    return q.tiles ? attend_only_item(a.s, q).units : 0;
-  else
-    return attend_units(a.s, q);
+__device__ __forceinline__ int units_of(const AttendArgs& a, const AttendRequest& q, int i, int lanes) {
+  if constexpr (ONE) return q.tiles ? attend_only_item(a.s, q).units : 0;
+  int n = 0;
+#pragma unroll 1
+  for (int t = i; t < q.tiles; t += lanes) n += attend_item(a.s, q, t).units;
+  return n;
 }
 
 // Every wave counts the units of all requests by itself, every lane those of some requests in a row: three loads and a scan without
@@ -125,24 +140,24 @@ __device__ __forceinline__ int units_of(const AttendArgs& a, const AttendRequest
 // inlined and unrolled 1000 instructions).
 template <bool ONE>
 __device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
-  const int lane = threadIdx.x & 63, R = (int)a.s.R, H = a.s.H, each = (R + 63) / 64;
+  const int lane = threadIdx.x & 63, R = (int)a.s.R, H = a.s.H, lanes = ONE ? 1 : a.s.lanes, log = __builtin_ctz(lanes), sub = lane & (lanes - 1);
+  const int each = (R + (64 >> log) - 1) >> (6 - log);
   int ctx = 0, start = 0, end = 0, mine = 0;
 #pragma unroll 1
   for (int i = 0; i < each; ++i) {
-    const int r = lane * each + i;
+    const int r = (lane >> log) * each + i;
+    int units = 0;
     if (r < R) {
       ctx = a.ctx_len[r];
       start = a.q_start ? a.q_start[r] : r;
       end = a.q_start ? a.q_start[r + 1] : r + 1;
-      mine = attend_sum(mine, units_of<ONE>(a, attend_request(a.s, ctx, start, end)) * H);
+      units = units_of<ONE>(a, attend_request(a.s, ctx, start, end), sub, lanes);
     }
+    if (!ONE) units = add_lanes(units, lanes);
+    mine = attend_sum(mine, units * H);
   }
-  int upto = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(upto, d);
-    if (lane >= d) upto = attend_sum(upto, y);
-  }
+  if (!ONE && sub) mine = 0;
+  const int upto = upto_lane(mine, lane);
   const int total = __builtin_amdgcn_readlane(upto, 63), line = uniform(attend_line(a.s, total));
   w.share = uniform(attend_share(a.s, line));
   w.begin = w.at = wg * w.share;
@@ -158,13 +173,14 @@ __device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
   // the lane whose requests hold the unit, and then the request
   const int owner = __builtin_ctzll(__ballot(off < upto));
   w.rest = off - (__builtin_amdgcn_readlane(upto, owner) - __builtin_amdgcn_readlane(mine, owner));
-  w.r = owner * each;
+  w.r = (owner >> log) * each;
   w.q = attend_request(a.s, __builtin_amdgcn_readlane(ctx, owner), __builtin_amdgcn_readlane(start, owner), __builtin_amdgcn_readlane(end, owner));
   int units = __builtin_amdgcn_readlane(mine, owner);
   if (each > 1) {
     for (;; ++w.r) {
       w.q = request(a, w.r);
-      units = uniform(units_of<ONE>(a, w.q) * H);
+      const int n = units_of<ONE>(a, w.q, ONE ? 0 : lane, 64);
+      units = uniform((ONE ? n : add_lanes(n, 64)) * H);
       if (w.rest < units) break;
       w.rest -= units;
     }
@@ -172,6 +188,19 @@ __device__ inline bool find(const AttendArgs& a, int wg, Walk& w) {
   units = uniform((int)((uint32_t)units / (uint32_t)H));
   w.h = uniform((int)((uint32_t)w.rest / (uint32_t)units));
   w.rest -= w.h * units;
+  // ... and the row tile, 64 at a time
+  if constexpr (!ONE) {
+    for (; w.t < w.q.tiles; w.t += 64) {
+      const int n = w.t + lane < w.q.tiles ? attend_item(a.s, w.q, w.t + lane).units : 0, sum = upto_lane(n, lane), all = __builtin_amdgcn_readlane(sum, 63);
+      if (w.rest < all) {
+        const int tile = __builtin_ctzll(__ballot(w.rest < sum));
+        w.rest -= __builtin_amdgcn_readlane(sum, tile) - __builtin_amdgcn_readlane(n, tile);
+        w.t += tile;
+        break;
+      }
+      w.rest -= all;
+    }
+  }
   return true;
 }
 
@@ -245,10 +274,10 @@ __device__ __forceinline__ int load_id(const AttendArgs& a, const int32_t* table
 // query tokens over 60000 268 -> 272), an fp16 call 0 to 2 % (1024 query tokens over 8192 256 either way, 64 requests of 12400 tokens 113 either way, 200
 // tokens of 20 queries 12.0 -> 12.3).
 struct Gate {
-  float room, times[2];
+  float room, times[4];
   int odd;
   bool low;
-  __device__ __forceinline__ Gate(float c) : room(kRoom), times{c, c}, odd(0), low(false) {}
+  __device__ __forceinline__ Gate(float c) : room(kRoom), times{c, c, c, c}, odd(0), low(false) {}
   __device__ __forceinline__ void see(bool large) {
     low = low || large;
     room = large ? -__builtin_inff() : room;

@@ -34,6 +34,7 @@ struct AttendShape {
   int32_t wgs;         // workgroups
   uint32_t inverse;    // n * inverse >> 16 is n / g for n below 32
   int32_t longest;     // units of a layer, at most
+  int32_t lanes;       // that count the row tiles of a request, a power of two up to 64
 };
 
 // A request's query tokens, row tiles and cached tokens, from what the device arrays hold (anything at all).
@@ -163,6 +164,15 @@ inline int64_t attend_most_units(const AttendShape& s) {
   return n < 1 ? 1 : n + s.free;
 }
 
+// Lanes of a wave that share the counting of a request's row tiles, so that a wave has counted all requests' soonest.
+inline int32_t attend_lanes(int64_t R, int64_t tiles) {
+  const auto turns = [&](int64_t n) { return ((R * n + 63) / 64) * ((tiles + n - 1) / n); };
+  int32_t best = 1;
+  for (int32_t n = 2; n <= 64; n *= 2)
+    if (turns(n) < turns(best)) best = n;
+  return best;
+}
+
 constexpr int64_t kMostTokens = 0x7fffffffLL / 2;  // query tokens of a layer, and requests
 
 // The shape of a call; false where it is beyond what the kernels count in 32 bits.
@@ -175,7 +185,7 @@ inline bool attend_shape(AttendShape* s, int64_t L, int64_t R, int64_t E, int32_
   const AttendKernel k = kernels(max_q * g, (double)L * R * H, E * T / 64);
   // a window longer than any position is none
   *s = {L, R, E, T, H, g, (int32_t)n_q, (int32_t)max_q, (int32_t)(window > 0x7fffffffLL ? 0 : window), k.rows, k.unit, (int32_t)(E * T), k.least, k.free, k.wgs,
-        65536u / (uint32_t)g + 1, (int32_t)(L > 0 ? (kLongestLine - 1) / L : 0)};
+        65536u / (uint32_t)g + 1, (int32_t)(L > 0 ? (kLongestLine - 1) / L : 0), attend_lanes(R, (max_q * g + k.rows - 1) / k.rows)};
   // a short table: items are not cut, and nothing has to be joined
   if (s->cap <= kWholeTokens) s->unit = (s->cap + k.unit - 1) / k.unit * k.unit + k.unit, s->least = 1, s->free = 0;
   // Row tiles of a layer and KV head: as many as every request's longest step has, but no more than all query tokens together fill (those of one

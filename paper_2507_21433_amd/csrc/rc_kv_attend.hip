@@ -11,6 +11,9 @@
 #include "rc_attend.hpp"
 #include "rc_kv.hpp"
 
+// Lambdas of a kernel work on its registers: one that were called instead would put them into memory.
+#define RC_INLINE __attribute__((always_inline))
+
 namespace rc {
 namespace {
 
@@ -37,22 +40,32 @@ struct KvLanes {
   }
 };
 // STREAM: tokens that no other workgroup reads are not kept in the caches behind this one, where there are too many of them anyway.
+typedef const __attribute__((address_space(1))) char* global_ptr;
 template <bool STREAM>
-__device__ __forceinline__ u32x4 load16(const char* p) {
+__device__ __forceinline__ u32x4 load16(global_ptr p) {
+  typedef const __attribute__((address_space(1))) u32x4* vector_ptr;
   if constexpr (STREAM)
-    return __builtin_nontemporal_load((const u32x4*)p);
+    return __builtin_nontemporal_load((vector_ptr)p);
   else
-    return *(const u32x4*)p;
+    return *(vector_ptr)p;
+}
+// An address that all lanes have in common, kept in scalar registers: left to the compiler, each lane's offset is added to the first part of it outside of
+// the loop, in vector registers.
+__device__ __forceinline__ global_ptr scalar(const char* p) {
+  asm volatile("" : "+s"(p));
+  return (global_ptr)p;
 }
 template <bool STREAM>
 __device__ __forceinline__ void load_k(KvTile& x, const char* k, const KvLanes& at) {
+  const global_ptr p = scalar(k);
 #pragma unroll
-  for (int d = 0; d < 4; ++d) x.k[d] = load16<STREAM>(k + at.k + d * 64);
+  for (int d = 0; d < 4; ++d) x.k[d] = load16<STREAM>(p + at.k + d * 64);
 }
 template <bool STREAM>
 __device__ __forceinline__ void load_v(KvTile& x, const char* v, const KvLanes& at) {
+  const global_ptr p = scalar(v);
 #pragma unroll
-  for (int r = 0; r < 4; ++r) x.v[r] = load16<STREAM>(v + at.v[r]);
+  for (int r = 0; r < 4; ++r) x.v[r] = load16<STREAM>(p + at.v[r]);
 }
 // Where the tile whose id lane j holds lies behind the layer's and head's first byte (its parity chooses between the halves of a block of 32); in block 0
 // where there is no such block (`there` false): its values are replaced or masked.
@@ -97,12 +110,12 @@ __device__ __forceinline__ uint32_t strange_half(uint32_t w) {
 // V of tokens that no row sees replaced by 0: whatever lies there (memory that was never written) gets a probability of 0, and 0 times infinity or NaN would
 // not be 0.  So are infinities and NaNs of tokens that only some rows may see: strange() adds them to these.  Token r of the lane stands at pos + r.  True if
 // there were such.
-template <bool BF16>
-__device__ inline bool seen_only(u32x4 (&v)[4], int pos, bool there, const AttendItem& it) {
+template <bool BF16, int N>
+__device__ inline bool seen_only(u32x4 (&v)[N], int pos, bool there, const AttendItem& it) {
   const uint32_t span = there ? it.high_max - it.low_min : 0;  // (an item that sees no token has no run)
   uint32_t found = 0;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
+  for (int r = 0; r < N; ++r) {
     const uint32_t keep = (uint32_t)(pos + r - it.low_min) < span ? ~0u : 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -114,19 +127,24 @@ __device__ inline bool seen_only(u32x4 (&v)[4], int pos, bool there, const Atten
   return found != 0;
 }
 // Infinities and NaNs of a tile's V (16 tokens from position pos on) into the sums of the rows that see them: the lane's row sees `span` positions from
-// low on.
-template <bool BF16>
+// low on.  o[c][r] is the sum of dim 32 * quarter + 8 r + c, FOURS: 4 c + r.
+template <bool BF16, bool FOURS>
 __device__ __forceinline__ void strange(f32x4 (&o)[8], const char* v, uint32_t token_b, int pos, int low, uint32_t span, int quarter) {
 #pragma unroll 1
   for (int t = 0; t < 16; ++t) {
     const bool seen = (uint32_t)(pos + t - low) < span;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
+      __builtin_amdgcn_sched_barrier(0);
       const u32x4 x = *(const u32x4*)(v + t * token_b + (4 * quarter + r) * 16);
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         const uint32_t w = x[c >> 1], bad = strange_half<BF16>(w);
-        if (seen && (c & 1 ? bad >> 16 : bad & 0xffffu)) o[c][r] += c & 1 ? high16<BF16>(w) : low16<BF16>(w);
+        const float add = seen && (c & 1 ? bad >> 16 : bad & 0xffffu) ? c & 1 ? high16<BF16>(w) : low16<BF16>(w) : 0.f;
+        if constexpr (FOURS)
+          o[2 * r + (c >> 2)][c & 3] += add;
+        else
+          o[c][r] += add;
       }
     }
   }
@@ -215,6 +233,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
       for (int j = 0; j < 2; ++j) load_k<STREAM>(x[j], head_k + at[j], lanes);
 #pragma unroll
       for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], head_v + at[j], lanes);
+      // (these loads and those at the loop's end would become one at its beginning, were there nothing different behind them)
+      asm volatile("; the first run is on its way" ::: "memory");
     }
     // The next run's K is on its way from where this one's is used up, and V likewise.  The loads are never left out (behind the
     // last run that one is loaded again): where a branch goes round them, a wait for some of the loads becomes a wait for all.
@@ -248,7 +268,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
               const bool is = (uint32_t)(pos + 16 * j + 4 * quarter + r - low[t]) < (there[j] ? span[t] : 0u);
               s[t][j][r] = is ? s[t][j][r] : -__builtin_inff();
             }
-            if (__builtin_expect(odd[j], 0)) strange<BF16>(o[t], head_v + here[j], a.token_b, pos + 16 * j, low[t], span[t], quarter);
+            if (__builtin_expect(odd[j], 0)) strange<BF16, false>(o[t], head_v + here[j], a.token_b, pos + 16 * j, low[t], span[t], quarter);
           }
         }
       }
@@ -302,6 +322,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], head_v + at[j], lanes);
+      asm volatile("; the next run is on its way" ::: "memory");
     }
 
     // the four waves' sums, under the largest of their references
@@ -358,25 +379,52 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
   }
 }
 
-// ---- Many rows: every wave has 32 of an item's 128 rows (16 of 64 with one row tile), and the workgroup lays 64 tokens at a time out as operands
-// in LDS, once for all of its rows: every wave 16 tokens, into the buffer that the step does not read.
+// ---- Many rows: every wave has 16 RT of an item's rows, and the workgroup takes runs of 32 tokens into LDS, once for all of its rows: straight from
+// memory, three runs ahead of the one that is computed.  K comes in operand order: a lane asks for the 16 bytes that it will hold.
+// V comes token by token, and reads that transpose give a lane four tokens of a dim; the 16-byte units of a token's 256 are exchanged by its
+// number (unit u lies at u ^ token % 4), so that the sixteen lanes of such a read, four tokens and four units of each, find different banks.
 
+constexpr int kRuns = 4;  // buffers
+
+template <int RT>
 struct ManyLds {
-  u32x4 k[2][4][4][64];     // [buffer][16 tokens][step of the dims][lane]
-  u32x2 v[2][2][8][64][2];  // [buffer][32 tokens][chunk][lane][16 tokens of the 32]
-  int32_t there[2][4];      // of the tiles of a buffer: whether there is a block (1), large V (16), infinities or NaNs that only some rows may see (32)
-  float ref[kWaves][32];    // references of odd row tiles
+  u32x4 k[kRuns][2][4][64];    // [buffer][16 tokens][step of the dims][lane]
+  u32x4 v[kRuns][2][4][64];    // [buffer][16 tokens][4 tokens][unit]
+  int32_t odd[kWaves];         // infinities or NaNs that only some rows may see, in the part of a run that a wave looked through
+  float ref[kWaves][16 * RT];  // references of odd row tiles
 };
+
+// 16 bytes a lane from memory into LDS, lane l's to to + 16 l, past the registers: counted by vmcnt, waited for by hand.
+__device__ __forceinline__ void to_lds(const char* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
+
+// Four tokens of a dim: lane 4 k + m of sixteen names dims 4 m' .. 4 m' + 3 of token k, lane l gets dim l % 4 of those that the lanes l / 4 named.
+__device__ __forceinline__ u32x2 read_transposed(uint32_t at) {
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s4* lds_ptr;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)at));
+}
+
+// Sums of this size and more of bf16 values might overflow, here or where parts are joined: the item is computed again under lower limits (rescale()).
+constexpr float kLargeSum = 0x1p100f;
 
 template <bool BF16, int RT>
 __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(KvAttendArgs a) {
-  constexpr int kStep = 64, kRows = kWaves * 16 * RT;
-  __shared__ ManyLds lds;
+  constexpr int kRows = kWaves * 16 * RT;
+  __shared__ ManyLds<RT> lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
-  const KvLanes lanes(a, lane);
   Walk w;
   if (!find<false>(a, wg, w)) return;
+  // A wave brings half of a run's K and V of 16 tokens: steps 2 part and the next of K's dims, tokens 8 part .. 8 part + 7 of V.
+  const int tile = wave >> 1, part = wave & 1;
+  const uint32_t from_k = col * a.token_b + quarter * 16 + part * 128, from_v = (8 * part + quarter) * a.token_b + (col ^ quarter) * 16;
+  // where the lane's transposed reads of chunk pairs begin: the four tokens of its quarter, token (lane / 4) % 4, unit 4 (lane % 4) + i
+  uint32_t read_at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) read_at[i] = lds_offset(&lds.v[0][0][quarter][(col >> 2) * 16 + (lane & 3) * 4 + (i ^ (col >> 2))]);
   for (;;) {
     Part cut;
     if (!take_part<false>(a, w, cut)) continue;
@@ -389,11 +437,10 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(KvAttendArgs a) {
       if (!go_on<false>(a, wg, w, cut)) return;
       continue;
     }
-    const int pa = cut.pa, pb = cut.pb;
     const int64_t head = (int64_t)w.l * a.layer_stride_b + w.h * 256;
     const char *head_k = a.k + head, *head_v = a.v + head;
     const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
-    const int steps = (pb - pa + 1) / 2, row0 = w.t * kRows + wave * 16 * RT;
+    const int mine = cut.pb - cut.pa, row0 = w.t * kRows + wave * 16 * RT;
     const bool busy = row0 < w.q.rows;
 
     u32x4 q[RT][4];
@@ -407,149 +454,180 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(KvAttendArgs a) {
       load_rows<false>(a, w, n, quarter, q[t]);
       const int pos = row_position<false>(a, w, n);
       low[t] = attend_low(a.s, pos), span[t] = max(attend_high(a.s, pos) - low[t], 0);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
-      ref[t] = kNothing, sum[t] = 0.f;
     }
+    // (waited for here: in the loop a wait for them would be one for the runs on their way as well)
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) asm volatile("" : "+v"(q[t][d]));
 
-    const auto at_ends = [&](int pos) { return pos < w.item.low_max || pos + kStep > w.item.high_min; };
     Gate gate(a.c);
-    // the wave's 16 tokens of a step
-    int ids = -1;
-    const auto load = [&](KvTile& x, bool& there, int step) {
-      if ((step & 63) == 0) {
-        const int pair = pa + 2 * (step + lane) + (wave >> 1);
-        ids = load_id(a, table, 2 * pair + (wave & 1), pair < pb);
+    // Runs whose blocks are all gone are passed over: block ids of 32 runs at a time, a bit of `left` for each that has a block.
+    int ids = -1, batch = -32;
+    uint64_t left = 0;
+    // of the runs in the buffers: position (-1: there is no further run), and whether its tiles have blocks (bits 0 and 1)
+    int pos[kRuns], there[kRuns];
+    const auto load = [&](int b) RC_INLINE {
+      pos[b] = -1;
+      while (left == 0) {
+        batch += 32;
+        if (batch >= mine) return;
+        const int pair = cut.pa + batch + (lane >> 1);
+        ids = load_id(a, table, 2 * pair + (lane & 1), pair < cut.pb);
+        const uint64_t x = __ballot(ids >= 0);
+        left = (x | x >> 1) & 0x5555555555555555ull;
       }
-      const uint64_t at = tile_offset(a, __builtin_amdgcn_readlane(ids, step & 63), wave & 1, there);
-      load_k<false>(x, head_k + at, lanes);
-      load_v<false>(x, head_v + at, lanes);
+      const int bit = __builtin_ctzll(left);
+      left &= left - 1;
+      pos[b] = (cut.pa + batch + (bit >> 1)) * kPairTokens;
+      const int id0 = __builtin_amdgcn_readlane(ids, bit), id1 = __builtin_amdgcn_readlane(ids, bit + 1);
+      there[b] = (id0 >= 0) | (id1 >= 0) << 1;
+      bool is;
+      const uint64_t at = tile_offset(a, tile ? id1 : id0, tile, is);
+      const uint32_t k = lds_offset(&lds.k[b][tile][2 * part][0]), v = lds_offset(&lds.v[b][tile][2 * part][0]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) to_lds(head_k + at, from_k + i * 64, k + i * 1024);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) to_lds(head_v + at, from_v + 4 * i * a.token_b, v + i * 1024);
     };
-    const auto lay = [&](KvTile& x, bool there, int step, int buf) {
-      const int pos = (pa + 2 * step) * kPairTokens;
-      int flags = there;
-      if (at_ends(pos) || !there) flags |= __any(seen_only<BF16>(x.v, pos + 16 * wave + 4 * quarter, there, w.item)) ? 32 : 0;
-      if constexpr (BF16) flags |= __any(large_bits(x.v) != 0) ? 16 : 0;
-      if (lane == 0) lds.there[buf][wave] = flags;
+    // What no row sees of the wave's part of a run, and what only some rows may see, is made 0 where it lies.  Bits of tiles with such.
+    const auto clean = [&](int b) RC_INLINE {
+      bool odd = false;
 #pragma unroll
-      for (int d = 0; d < 4; ++d) lds.k[buf][wave][d][lane] = x.k[d];
-      const auto chunks = [&](auto b) {
-        constexpr int B = decltype(b)::value;
-        uint32_t e[2], d[2];
-        pair_v<B>(x.v, e, d);
-        lds.v[buf][wave >> 1][2 * B][lane][wave & 1] = u32x2{e[0], e[1]};
-        lds.v[buf][wave >> 1][2 * B + 1][lane][wave & 1] = u32x2{d[0], d[1]};
-      };
-      chunks(std::integral_constant<int, 0>{});
-      chunks(std::integral_constant<int, 1>{});
-      chunks(std::integral_constant<int, 2>{});
-      chunks(std::integral_constant<int, 3>{});
+      for (int i = 0; i < 2; ++i) {
+        u32x4* p = &lds.v[b][tile][2 * part + i][lane];
+        u32x4 one[1] = {*p};
+        odd |= seen_only<BF16>(one, pos[b] + 16 * tile + 4 * (2 * part + i) + quarter, there[b] >> tile & 1, w.item);
+        *p = one[0];
+      }
+      const bool any = __any(odd);
+      if (lane == 0) lds.odd[wave] = any;
+      __syncthreads();
+      return uniform((lds.odd[0] | lds.odd[1]) | (lds.odd[2] | lds.odd[3]) << 1);
     };
-    const auto attend = [&](int step, int buf) {
-      const int pos = (pa + 2 * step) * kPairTokens;
-      // Operands come from LDS four at a time, while the products of the four before them run: left to the compiler, every read is
-      // waited for by itself.
-      f32x4 s[RT][4];
+    const auto attend = [&](int b, bool masked, int odd) RC_INLINE {
+      f32x4 s[RT][2];
+      // Operands come from LDS ahead of their products: left to the compiler, nearly every read is waited for by itself.
+      u32x4 k[2][2];
+      const auto read_k = [&](int d) RC_INLINE {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) s[t][j] = f32x4{0, 0, 0, 0};
-      u32x4 k[2][4];
-      const auto read_k = [&](int i) {  // tiles 2 (i / 2) and the next, steps 2 (i % 2) and the next
-#pragma unroll
-        for (int m = 0; m < 4; ++m) k[i & 1][m] = lds.k[buf][(i & 2) + (m & 1)][2 * (i & 1) + (m >> 1)][lane];
+        for (int j = 0; j < 2; ++j) k[d & 1][j] = lds.k[b][j][d][lane];
       };
       read_k(0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i < 3) read_k(i + 1);
+      for (int d = 0; d < 4; ++d) {
+        if (d < 3) read_k(d + 1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int t = 0; t < RT; ++t) s[t][(i & 2) + (m & 1)] = mfma<BF16>(k[i & 1][m], q[t][2 * (i & 1) + (m >> 1)], s[t][(i & 2) + (m & 1)]);
+          for (int t = 0; t < RT; ++t) s[t][j] = mfma<BF16>(k[d & 1][j], q[t][d], d ? s[t][j] : f32x4{0, 0, 0, 0});
         __builtin_amdgcn_sched_barrier(0);
       }
-      int f[4], all = 15, any = 0;
+      if (__builtin_expect(masked, 0)) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = uniform(lds.there[buf][j]), any |= f[j], all &= f[j];
-      if constexpr (BF16) gate.see((any & 16) != 0);
-      if (at_ends(pos) || !(all & 1)) {
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const bool is = (uint32_t)(pos + 16 * j + 4 * quarter + r - low[t]) < (f[j] & 1 ? span[t] : 0u);
+              const bool is = (uint32_t)(pos[b] + 16 * j + 4 * quarter + r - low[t]) < (there[b] >> j & 1 ? span[t] : 0u);
               s[t][j][r] = is ? s[t][j][r] : -__builtin_inff();
             }
-        }
-        if (__builtin_expect(any & 32, 0)) {
 #pragma unroll 1
-          for (int j = 0; j < 4; ++j) {
-            if (!(uniform(lds.there[buf][j]) & 32)) continue;
-            bool there;
-            const int tile = 2 * (pa + 2 * step) + j;
-            const uint64_t at = tile_offset(a, uniform(load_id(a, table, tile, true)), tile & 1, there);
+        for (int j = 0; odd >> j; ++j) {
+          if (!(odd >> j & 1)) continue;
+          bool is;
+          const uint64_t at = tile_offset(a, uniform(load_id(a, table, pos[b] / 16 + j, true)), j, is);
 #pragma unroll
-            for (int t = 0; t < RT; ++t) strange<BF16>(o[t], head_v + at, a.token_b, pos + 16 * j, low[t], span[t], quarter);
-          }
+          for (int t = 0; t < RT; ++t) strange<BF16, true>(o[t], head_v + at, a.token_b, pos[b] + 16 * j, low[t], span[t], quarter);
         }
       }
+      float top[RT];
+      bool over = false;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        float top = s[t][0][0];
+        top[t] = s[t][0][0];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j >> 2][j & 3]);
-        rescale<BF16>(s[t], o[t], ref[t], sum[t], top, a.c, t, gate, lds.ref[wave][16 * t + col]);
+        for (int j = 0; j < 8; ++j) top[t] = fmaxf(top[t], s[t][j >> 2][j & 3]);
+        over |= fmaf(top[t], gate.times[t], -ref[t]) > gate.room;
       }
-      u32x4 v[8], p16[RT][2];
-      const auto read_v = [&](int i) {  // the chunks of tokens 32 i and the next
+      if (__builtin_expect(__any(over), 0)) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] = *(const u32x4*)&lds.v[buf][i][c][lane][0];
-      };
-      const auto weigh = [&](int i) {
+        for (int t = 0; t < RT; ++t) rescale<BF16>(s[t], o[t], ref[t], sum[t], top[t], a.c, t, gate, lds.ref[wave][16 * t + col]);
+      }
+      u32x4 v[2][4], p16[RT];
+      const auto read_v = [&](int i) RC_INLINE {  // chunks 4 i to 4 i + 3
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          float p[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + (j >> 2)][j & 3], gate.times[t], -ref[t]));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) p16[t][i][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
-          sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t at = read_at[2 * i + (c >> 1)] + b * (uint32_t)sizeof(lds.v[0]) + (c & 1) * 8;
+          const u32x2 x = read_transposed(at), y = read_transposed(at + (uint32_t)sizeof(lds.v[0][0]));
+          v[i][c] = u32x4{x[0], x[1], y[0], y[1]};
         }
       };
-      const auto add = [&](int i) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int t = 0; t < RT; ++t) o[t][c] = mfma<BF16>(v[c], p16[t][i], o[t][c]);
-      };
       read_v(0);
-      weigh(0);
-      add(0);
-      weigh(1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[t][j >> 2][j & 3], gate.times[t], -ref[t]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p16[t][j] = pack2<BF16>(p[2 * j], p[2 * j + 1]);
+        sum[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
       read_v(1);
-      add(1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) o[t][c] = mfma<BF16>(v[c >> 2][c & 3], p16[t], o[t][c]);
     };
 
-    KvTile x;
-    bool there;
-    if (steps > 0) {
-      load(x, there, 0);
-      lay(x, there, 0, 0);
-    }
-    __syncthreads();
-    // behind the last step a tile of no block is loaded and laid into the buffer that is free
-    for (int step = 0; step < steps; ++step) {
-      load(x, there, step + 1);
-      if (busy) attend(step, step & 1);
-      lay(x, there, step + 1, ~step & 1);
+    for (;;) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) o[t][c] = f32x4{0, 0, 0, 0};
+        ref[t] = kNothing, sum[t] = 0.f;
+      }
+      ids = -1, batch = -32, left = 0;
+      // (the buffers are free: whoever read them last has passed a barrier since, or is behind the loop's last one and reads no more)
       __syncthreads();
+#pragma unroll
+      for (int b = 0; b + 1 < kRuns; ++b) load(b);
+      bool more = true;
+      while (more) {
+#pragma unroll
+        for (int b = 0; b < kRuns; ++b) {
+          if (pos[b] < 0) {
+            more = false;
+            break;
+          }
+          // this run has landed where the two behind it may still be on their way, and nobody reads the buffer before it any more
+          if (pos[(b + 2) % kRuns] >= 0)
+            asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          load((b + 3) % kRuns);
+          const bool masked = pos[b] < w.item.low_max || pos[b] + kPairTokens > w.item.high_min || there[b] != 3;
+          const int odd = masked ? clean(b) : 0;
+          if (busy) attend(b, masked, odd);
+        }
+      }
+      if constexpr (!BF16) break;
+      bool large = false;
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) large |= !(fabsf(o[t][i >> 2][i & 3]) < kLargeSum);
+      if (gate.low || !__syncthreads_or(large && busy)) break;
+      gate = Gate(a.c);
+      gate.see(true);
     }
 
-    float* part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(kRows));
+    float* to_part = (float*)(a.parts + attend_place(wg, w.at == w.begin) * (int64_t)attend_part_bytes(kRows));
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const float all = row_sum(sum[t]);
@@ -560,19 +638,16 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(KvAttendArgs a) {
         const float f = row_scale(all);
         const int64_t place = row_place<false>(a, w, n);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          *(u32x4*)(a.out + (place * 128 + (4 * quarter + r) * 8) * 2) =
-              u32x4{pack2<BF16>(o[t][0][r] * f, o[t][1][r] * f), pack2<BF16>(o[t][2][r] * f, o[t][3][r] * f),
-                    pack2<BF16>(o[t][4][r] * f, o[t][5][r] * f), pack2<BF16>(o[t][6][r] * f, o[t][7][r] * f)};
+        for (int i = 0; i < 4; ++i)
+          *(u32x4*)(a.out + (place * 128 + quarter * 32 + i * 8) * 2) =
+              u32x4{pack2<BF16>(o[t][2 * i][0] * f, o[t][2 * i][1] * f), pack2<BF16>(o[t][2 * i][2] * f, o[t][2 * i][3] * f),
+                    pack2<BF16>(o[t][2 * i + 1][0] * f, o[t][2 * i + 1][1] * f), pack2<BF16>(o[t][2 * i + 1][2] * f, o[t][2 * i + 1][3] * f)};
         if (quarter == 0 && a.lse) a.lse[place] = row_lse(ref[t], all);
         if (quarter == 0 && a.ends) a.ends[place] = float2{ref[t], all};
       } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          *(f32x4*)(part + m * 128 + (4 * quarter + r) * 8) = f32x4{o[t][0][r], o[t][1][r], o[t][2][r], o[t][3][r]};
-          *(f32x4*)(part + m * 128 + (4 * quarter + r) * 8 + 4) = f32x4{o[t][4][r], o[t][5][r], o[t][6][r], o[t][7][r]};
-        }
-        if (quarter == 0) part[kRows * 128 + m * 2] = ref[t], part[kRows * 128 + m * 2 + 1] = all;
+        for (int c = 0; c < 8; ++c) *(f32x4*)(to_part + m * 128 + quarter * 32 + c * 4) = o[t][c];
+        if (quarter == 0) to_part[kRows * 128 + m * 2] = ref[t], to_part[kRows * 128 + m * 2 + 1] = all;
       }
     }
     if (!go_on<false>(a, wg, w, cut)) return;
@@ -629,26 +704,38 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
     float sum[kWeighTiles];
 #pragma unroll
     for (int j = 0; j < kWeighTiles; ++j) sum[j] = 0.f;
-    const int row_tiles = (w.q.rows + 15) / 16, from = (int)((int64_t)row_tiles * share / g.shares), to = (int)((int64_t)row_tiles * (share + 1) / g.shares);
-#pragma unroll 1
-    for (int t = from; t < to; ++t) {
-      const int n = t * 16 + col, n_last = min(t * 16 + 15, w.q.rows - 1);
-      const int p0 = first + t * 16 / a.s.g, p1 = first + n_last / a.s.g;
-      if (attend_high(a.s, p1) <= pos0 || attend_low(a.s, p0) >= pos0 + kWeighTiles * 16) continue;
+    // the row tiles that see any of these tokens, and the task's share of them
+    const int g_ = a.s.g, end = pos0 + kWeighTiles * 16;
+    const int64_t beyond = a.s.window ? ((int64_t)end + a.s.window - 1 - first) * g_ : w.q.rows;
+    const int t0 = pos0 > first ? (int)((int64_t)(pos0 - first) * g_ / 16) : 0, t1 = (int)((min(beyond, (int64_t)w.q.rows) + 15) / 16);
+    const int from = t0 + (int)((int64_t)(t1 - t0) * share / g.shares), to = t0 + (int)((int64_t)(t1 - t0) * (share + 1) / g.shares);
+    struct Rows {
       u32x4 q[4];
-      load_rows<false>(a, w, n, quarter, q);
-      float2 end = {0.f, 0.f};
-      if (n < w.q.rows) end = a.ends[row_place<false>(a, w, n)];
-      const float f = row_scale(end.y);
-      const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) < pos0 + kWeighTiles * 16 || there != 255;
-      const int pos = first + min(n, w.q.rows - 1) / a.s.g, low = attend_low(a.s, pos);
-      const uint32_t span = max(attend_high(a.s, pos) - low, 0);
-      const bool coarse = uniform(__any(f != 0.f && fabsf(end.x) > kCoarse));
+      float2 end;
+      int pos;
+    };
+    const auto load = [&](Rows& x, int t) RC_INLINE {
+      const int n = t * 16 + col, m = min(n, w.q.rows - 1), j = (int)((uint32_t)m / (uint32_t)g_), row = w.h * g_ + m - j * g_;
+      x.pos = first + j;
+      x.end = a.ends[((int64_t)w.l * a.s.n_q + w.q.first + j) * (int64_t)(a.s.H * g_) + row];
+      const char* p = a.q + (int64_t)w.l * a.q_layer_stride_b + (int64_t)(w.q.first + j) * a.q_token_stride_b + row * 256 + quarter * 16;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) x.q[d] = *(const u32x4*)(p + d * 64);
+    };
+    const auto add_rows = [&](const Rows& x, int t) RC_INLINE {
+      const int p0 = first + t * 16 / g_, p1 = first + min(t * 16 + 15, w.q.rows - 1) / g_;
+      // a row that is not there, or that sees nothing: no weight, and a reference that no score comes near
+      const bool none = t * 16 + col >= w.q.rows || x.end.y == 0.f;
+      const float f = none ? 0.f : 1.f / x.end.y, ref = none ? -kNothing : x.end.x;
+      const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) < end || there != 255;
+      const int low = attend_low(a.s, x.pos);
+      const uint32_t span = max(attend_high(a.s, x.pos) - low, 0);
+      const bool coarse = uniform(__any(f != 0.f && fabsf(ref) > kCoarse));
 #pragma unroll
       for (int j = 0; j < kWeighTiles; ++j) {
         f32x4 s = {0, 0, 0, 0};
 #pragma unroll
-        for (int d = 0; d < 4; ++d) s = mfma<BF16>(k[j][d], q[d], s);
+        for (int d = 0; d < 4; ++d) s = mfma<BF16>(k[j][d], x.q[d], s);
         if (ends) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -659,18 +746,26 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
         float p[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float e = fmaf(s[r], a.c, -end.x);
-          if (coarse) {
+          float e = fmaf(s[r], a.c, -ref);
+          if (__builtin_expect(coarse, 0)) {
 #pragma clang fp contract(off)
-            const float z = s[r] * a.c, d = z - end.x;
-            e = fabsf(end.x) > kCoarse ? d : e;
+            const float z = s[r] * a.c, d = z - ref;
+            e = fabsf(ref) > kCoarse ? d : e;
           }
           p[r] = __builtin_amdgcn_exp2f(e);
         }
-        // a row that sees nothing has no weights (f is 0, and what it would be multiplied with need not be a number)
-        const float add = ((p[0] + p[1]) + (p[2] + p[3])) * f;
-        sum[j] += f == 0.f ? 0.f : add;
+        sum[j] = fmaf((p[0] + p[1]) + (p[2] + p[3]), f, sum[j]);
       }
+    };
+    // the next rows are on their way beside the products of these
+    Rows x, y;
+    if (from < to) load(x, from);
+#pragma unroll 1
+    for (int t = from; t < to; t += 2) {
+      load(y, min(t + 1, to - 1));
+      add_rows(x, t);
+      load(x, min(t + 2, to - 1));
+      if (t + 1 < to) add_rows(y, t + 1);
     }
     float* sums = g.sums + ((((int64_t)share * a.s.L + w.l) * a.s.R + w.r) * a.s.H + w.h) * (int64_t)g.tiles + chunk * kWeighTiles;
 #pragma unroll
@@ -731,6 +826,14 @@ __global__ __launch_bounds__(kThreads) void weigh_entries_kernel(WeighArgs g) {
 
 // ---- The call.
 
+inline AttendKernel kv_kernel(int64_t rows, double pairs, int64_t steps) {
+  if (rows <= 16) return {16, 128, 768, 4, 2};
+  if (rows <= 32) return {32, 128, 512, 4, 1};
+  const double tiles = pairs * (double)((rows + 127) / 128);
+  if (rows <= 64 || (tiles <= 128 && tiles * (double)steps <= 8192)) return {64, 64, 512, 8, 1};
+  return {192, 64, 512, 8, 3};
+}
+
 // What the workspace holds behind the parts of cut items, where blocks are weighed.
 struct WeighRoom {
   int64_t ends, gathered, sums;  // bytes
@@ -764,7 +867,7 @@ rc_status kv_check(const rc_kv_desc* d, int64_t n_blocks, int64_t R, int64_t E, 
   if (n_heads < 1 || n_heads % d->n_kv_heads != 0)
     return fail(RC_ERR_INVALID_ARG, "%s: n_heads %d is not a multiple of n_kv_heads %d", who, n_heads, d->n_kv_heads);
   if (n_heads > 1024) return fail(RC_ERR_UNSUPPORTED, "%s: n_heads %d (at most 1024)", who, n_heads);
-  if (!attend_shape(s, d->n_layers, R, n_blocks ? E : 0, d->block_tokens, d->n_kv_heads, n_heads, n_q, max_q, window))
+  if (!attend_shape(s, d->n_layers, R, n_blocks ? E : 0, d->block_tokens, d->n_kv_heads, n_heads, n_q, max_q, window, kv_kernel))
     return fail(RC_ERR_UNSUPPORTED, "%s: a table of 2^31 positions or more, or more than 2^30 query tokens, requests or row tiles", who);
   if (weigh && (double)d->n_layers * R * E > (double)kMostEntries) return fail(RC_ERR_UNSUPPORTED, "%s: more than 2^29 table entries to weigh", who);
   return RC_OK;
@@ -795,13 +898,13 @@ void kv_launch(const WeighArgs& g, hipStream_t st) {
   else if (a.s.rows == 64)
     kv_many_kernel<BF16, 1><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
   else
-    kv_many_kernel<BF16, 2><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
+    kv_many_kernel<BF16, 3><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
   if (a.borders) {
     const int64_t rows = (int64_t)a.s.max_q * a.s.g;
     if (few)
       attend_join_kernel<BF16, true><<<dim3(a.s.wgs - 1, (unsigned)(rows < a.s.rows ? rows : a.s.rows)), kThreads, 0, st>>>(a);
     else
-      attend_join_kernel<BF16, false><<<dim3(a.s.wgs - 1, 8), kThreads, 0, st>>>(a);
+      attend_join_kernel<BF16, false><<<dim3(a.s.wgs - 1, (a.s.rows + 15) / 16), kThreads, 0, st>>>(a);
   }
   if (!g.out) return;
   const int64_t entries = a.s.L * a.s.R * a.s.E;
@@ -830,7 +933,7 @@ extern "C" size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_
   const int64_t q = max_q < 1 ? max_q : 1;
   if (n_q < 0) return 0;
   if (kv_check(desc, n_blocks, R, E, n_heads, q, q, 0, weigh != 0, &s, "rc_kv_attend_workspace_size")) return 0;
-  size_t n = attend_largest_workspace(s.L, R, s.E, s.T, s.H, n_heads, max_q);
+  size_t n = attend_largest_workspace(s.L, R, s.E, s.T, s.H, n_heads, max_q, kv_kernel);
   if (weigh && max_q > 0) {
     if ((double)s.L * n_q * n_heads > 1e15) return 0;
     const int64_t runs = runs_of(s), few = max_q < kFewRows / s.g ? max_q : kFewRows / s.g;

@@ -700,27 +700,40 @@ def rc_kv_attend(q, k, v, tables, ctx_len, q_start=None, max_q=None, scale=None,
     return dict(out=out, lse=lse, weights=weights_out)
 
 
+@_by_layout
+def _kv_evict_layout(t, ts, tt, w, ws, wt, x, xs, xt, p, ps, pt, r, rs, rt):
+    assert tt == torch.int32 and len(t) == 3 and _contiguous(t, ts), "tables are int32 [L][R][E]"
+    assert wt == torch.float32 and w == t and _contiguous(w, ws), "weights are float32 [L][R][E]"
+    L, R, E = t
+    assert xt == pt == torch.int32 and x == p == (R,) and _contiguous(x, xs) and _contiguous(p, ps)
+    assert rt == torch.int32 and len(r) == 2 and r[0] == L and _contiguous(r, rs), "refcount is int32 [L][NB]"
+    return L, R, E, r[1]
+
+
+@_by_layout
+def _kv_evict_out(t, r, o, os_, ot, c, cs, ct, n, ns, nt):
+    assert ot == torch.int32 and o == t and _contiguous(o, os_)
+    assert ct == torch.int32 and c == r and _contiguous(c, cs)
+    assert nt == torch.int32 and n == t[:2] and _contiguous(n, ns)
+
+
 def rc_kv_evict(tables, weights, ctx_len, keep, refcount, block_tokens, n_first=1, n_last=1, in_place=False, out=None):
     """Table entries [L][R][E] beyond keep (int32 [R]) blocks a request leave, those of the smallest weights (float32 [L][R][E]) first; the first
     n_first and last n_last used ones stay.  Returns dict(tables, refcount [L][NB], n_evicted int32 [L][R])."""
-    _dev(tables, weights, ctx_len, keep, refcount)
-    assert tables.dtype == torch.int32 and tables.dim() == 3 and tables.is_contiguous(), "tables are int32 [L][R][E]"
-    L, R, E = tables.shape
-    assert weights.dtype == torch.float32 and weights.shape == tables.shape and weights.is_contiguous(), "weights are float32 [L][R][E]"
-    for t in (ctx_len, keep):
-        assert t.dtype == torch.int32 and t.shape == (R,) and t.is_contiguous()
-    assert refcount.dtype == torch.int32 and refcount.dim() == 2 and refcount.shape[0] == L and refcount.is_contiguous(), "refcount is int32 [L][NB]"
+    L, R, E, NB = _kv_evict_layout(tables.shape, tables.stride(), tables.dtype, weights.shape, weights.stride(), weights.dtype, ctx_len.shape,
+                                   ctx_len.stride(), ctx_len.dtype, keep.shape, keep.stride(), keep.dtype, refcount.shape, refcount.stride(), refcount.dtype)
     if out is not None:
         assert not in_place
         t_out, r_out, n_evicted = out["tables"], out["refcount"], out["n_evicted"]
-        _dev(t_out, r_out, n_evicted)
-        assert t_out.dtype == torch.int32 and t_out.shape == tables.shape and t_out.is_contiguous()
-        assert r_out.dtype == torch.int32 and r_out.shape == refcount.shape and r_out.is_contiguous()
-        assert n_evicted.dtype == torch.int32 and n_evicted.shape == (L, R) and n_evicted.is_contiguous()
+        _kv_evict_out(tables.shape, refcount.shape, t_out.shape, t_out.stride(), t_out.dtype, r_out.shape, r_out.stride(), r_out.dtype, n_evicted.shape,
+                      n_evicted.stride(), n_evicted.dtype)
     else:
         t_out = tables if in_place else torch.empty_like(tables)
         r_out = refcount if in_place else torch.empty_like(refcount)
         n_evicted = torch.empty((L, R), dtype=torch.int32, device=tables.device)
-    _check(lib().rc_kv_evict(L, _ptr(tables), _ptr(t_out), R, E, refcount.shape[1], int(block_tokens), _ptr(ctx_len), _ptr(weights), _ptr(keep),
-                             int(n_first), int(n_last), _ptr(refcount), _ptr(r_out), _ptr(n_evicted), _stream()))
+    _dev(tables, weights, ctx_len, keep, refcount, t_out, r_out, n_evicted)
+    code = lib().rc_kv_evict(L, tables.data_ptr(), t_out.data_ptr(), R, E, NB, block_tokens, ctx_len.data_ptr(), weights.data_ptr(), keep.data_ptr(), n_first,
+                             n_last, refcount.data_ptr(), r_out.data_ptr(), n_evicted.data_ptr(), _stream())
+    if code:
+        _check(code)
     return dict(tables=t_out, refcount=r_out, n_evicted=n_evicted)

@@ -56,68 +56,117 @@ struct EvictArgs {
   const int32_t *ctx_len, *keep;
   const float* weights;
   int64_t n_first, n_last;
+  const int32_t* copied;  // what the only workgroup copies to refcount first, or NULL
   int32_t *refcount, *n_evicted;
 };
 
 // The order of weights as that of whole numbers: -0 and 0 are equal, NaN is the largest.  What may not leave comes behind them all.
 constexpr uint32_t kStays = 0xffffffffu;
+constexpr int kSmallRow = 1024;  // entries of a row that one wave takes
 __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t b = __float_as_uint(w + 0.f);
   if (w != w) return kStays - 1;
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 
-// A row is the table of one request in one layer.  Its keys lie in registers where they fit (entry i * threads + thread at place i), else they are read
-// again for every pass.  The n-th smallest key is found byte by byte from the top with a histogram of the entries that agree so far; of those equal to
-// it the first ones leave.
+// A row is the table of one request in one layer.  The n entries that leave are those whose keys lie below a border, and of those that equal it the ones that
+// lie before a place of the table: both are found bit by bit from the top, with a count of the entries below at every bit.  Keys lie in registers (entry
+// i * threads + thread at place i), so that a count is a compare and a ballot for each; a row that they do not hold is counted by a histogram of
+// each byte in turn, for which it is read again.
 template <int WAVES, int ITEMS>  // ITEMS: entries of a thread held in registers, 0: none
 struct EvictRow {
   static constexpr int kRowThreads = 64 * WAVES;
   const EvictArgs& a;
   const int32_t* in;
   const float* weights;
-  int32_t E;
-  int32_t used, thread;
-  uint32_t* histogram;  // LDS, 256
-  uint32_t* scratch;    // LDS, 16 + a few
+  int32_t E, used, thread;
+  uint32_t* lds;  // 2 * WAVES sums, and 256 more without registers
+  int turn;
   uint32_t key[ITEMS ? ITEMS : 1];
-  int32_t id[ITEMS ? ITEMS : 1];
 
-  __device__ __forceinline__ void sync() const {
-    if constexpr (WAVES > 1)
-      __syncthreads();
-    else
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
   __device__ __forceinline__ bool held(int32_t i, int32_t e) const { return e < used && i >= 0 && i < a.NB; }
   __device__ __forceinline__ uint32_t make_key(int32_t i, int32_t e) const {
     return held(i, e) && e >= a.n_first && e < used - a.n_last ? weight_key(weights[e]) : kStays;
   }
-  // f(place, entry, id, key) for every entry of the thread; the same number of turns for all lanes of the row.
+  // Of a number of every wave, the same for all its lanes.
+  __device__ __forceinline__ uint32_t sum_waves(uint32_t x) {
+    if constexpr (WAVES == 1) return x;
+    uint32_t* at = lds + (turn++ & 1) * WAVES;  // (so that one barrier is enough: who still reads the last sums has not passed the next one)
+    if ((thread & 63) == 0) at[thread >> 6] = x;
+    __syncthreads();
+    x = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) x += at[i];
+    return __builtin_amdgcn_readfirstlane(x);
+  }
+  // f(entry, key) of every entry of the thread; the same number of turns for all lanes of the row.
   template <class F>
   __device__ __forceinline__ void each(F f) {
     if constexpr (ITEMS) {
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i)
-        if (i * kRowThreads < E) f(i * kRowThreads + thread, id[i], key[i]);
+        if (i * kRowThreads < E) f(i * kRowThreads + thread, key[i]);
     } else {
       for (int32_t base = 0; base < E; base += kRowThreads) {
-        const int32_t e = base + thread, j = e < E ? in[e] : -1;
-        f(e, j, make_key(j, e));
+        const int32_t e = base + thread;
+        f(e, make_key(e < E ? in[e] : -1, e));
       }
     }
   }
-  __device__ __forceinline__ uint32_t sum(uint32_t x) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-    if constexpr (WAVES > 1) {
-      if ((thread & 63) == 0) scratch[thread >> 6] = x;
+  template <class F>
+  __device__ __forceinline__ uint32_t count(F f) {
+    uint32_t n = 0;
+    each([&](int32_t e, uint32_t k) { n += __popcll(__ballot(f(e, k))); });
+    return sum_waves(n);
+  }
+  // The largest border of which fewer than n of the numbers x(entry, key) (in 32 bits, from `top` bits down) lie below; one with exactly n below it ends the
+  // search.
+  template <class F>
+  __device__ __forceinline__ uint32_t border(int top, uint32_t n, bool& exact, F below) {
+    uint32_t b = 0;
+    exact = false;
+#pragma unroll 1
+    for (int bit = top - 1; bit >= 0 && !exact; --bit) {
+      const uint32_t mid = b | 1u << bit, c = count([&](int32_t e, uint32_t k) { return below(e, k, mid); });
+      if (c <= n) b = mid, exact = c == n;
+    }
+    return b;
+  }
+  // The n-th smallest key by bytes, and how many of those that equal it leave.
+  __device__ __forceinline__ uint32_t nth(uint32_t n, uint32_t& equal) {
+    uint32_t *histogram = lds + 2 * WAVES, prefix = 0, mask = 0;
+    equal = n;
+#pragma unroll 1
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      if (thread < 256) histogram[thread] = 0;
       __syncthreads();
-      x = 0;
-      for (int i = 0; i < WAVES; ++i) x += scratch[i];
+      each([&](int32_t, uint32_t k) { if (k != kStays && (k & mask) == prefix) atomicAdd(&histogram[k >> shift & 255], 1u); });
+      __syncthreads();
+      // every wave finds the byte by itself: four bins a lane
+      const int lane = thread & 63;
+      const uint4 h = *(const uint4*)&histogram[4 * lane];
+      const uint32_t four = h.x + h.y + h.z + h.w;
+      uint32_t upto = four;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t y = __shfl_up(upto, d);
+        if (lane >= d) upto += y;
+      }
+      const int owner = __builtin_ctzll(__ballot(upto >= equal));
+      uint32_t before = upto - four, byte = 4 * lane;
+      if (before + h.x < equal) {
+        before += h.x, ++byte;
+        if (before + h.y < equal) {
+          before += h.y, ++byte;
+          if (before + h.z < equal) before += h.z, ++byte;
+        }
+      }
+      equal -= __builtin_amdgcn_readlane(before, owner);
+      prefix |= (uint32_t)__builtin_amdgcn_readlane(byte, owner) << shift;
+      mask |= 255u << shift;
       __syncthreads();
     }
-    return x;
+    return prefix;
   }
 };
 
@@ -125,90 +174,67 @@ template <int WAVES, int ITEMS>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void kv_evict_kernel(EvictArgs a) {
   constexpr int kRows = WAVES == 1 ? 4 : 1;
   using Row = EvictRow<WAVES, ITEMS>;
-  __shared__ __attribute__((aligned(16))) uint32_t histogram[kRows][256], scratch[kRows][32];
+  __shared__ __attribute__((aligned(16))) uint32_t lds[2 * WAVES + (ITEMS ? 0 : 256)];
   const int in_block = WAVES == 1 ? (int)(threadIdx.x >> 6) : 0;
+  if (a.copied) {
+    for (int64_t i = threadIdx.x; i < a.L * a.NB; i += blockDim.x) a.refcount[i] = a.copied[i];
+    __threadfence();
+    __syncthreads();
+  }
   const int64_t lr = (int64_t)blockIdx.x * kRows + in_block;
   if (lr >= a.L * a.R) return;
   const int64_t l = lr / a.R, r = lr - l * a.R;
-  Row row{a, a.tables_in + lr * a.E, a.weights + lr * a.E, (int32_t)a.E, 0, (int)(WAVES == 1 ? threadIdx.x & 63 : threadIdx.x), histogram[in_block], scratch[in_block], {}, {}};
+  Row row{a, a.tables_in + lr * a.E, a.weights + lr * a.E, (int32_t)a.E, 0, (int)(WAVES == 1 ? threadIdx.x & 63 : threadIdx.x), lds, 0, {}};
   int32_t* out = a.tables_out + lr * a.E;
-  const int32_t ctx = a.ctx_len[r], keep = a.keep[r];
+  const int32_t ctx = a.ctx_len[r], keep = max(a.keep[r], 0);
   const int64_t blocks = ctx > 0 ? ((int64_t)ctx + a.T - 1) / a.T : 0;
   row.used = (int32_t)(blocks < a.E ? blocks : a.E);
+  uint32_t held = 0;
   if constexpr (ITEMS) {
+    int32_t id[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int32_t e = i * Row::kRowThreads + row.thread;
-      row.id[i] = e < row.E ? row.in[e] : -1;
+      id[i] = e < row.E ? row.in[e] : -1;
     }
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) row.key[i] = row.make_key(row.id[i], i * Row::kRowThreads + row.thread);
+    for (int i = 0; i < ITEMS; ++i) {
+      const int32_t e = i * Row::kRowThreads + row.thread;
+      row.key[i] = row.make_key(id[i], e);
+      held += __popcll(__ballot(row.held(id[i], e)));
+    }
+    held = row.sum_waves(held);
+  } else {
+    held = row.count([&](int32_t e, uint32_t) { return e < row.E && row.held(row.in[e], e); });
   }
-  uint32_t held = 0, may = 0;
-  row.each([&](int32_t e, int32_t i, uint32_t k) { held += row.held(i, e), may += k != kStays; });
-  held = row.sum(held), may = row.sum(may);
-  uint32_t n = held > (uint32_t)max(keep, 0) ? held - (uint32_t)max(keep, 0) : 0;
-  n = min(n, may);
+  const uint32_t may = row.count([](int32_t, uint32_t k) { return k != kStays; });
+  const uint32_t n = min(held > (uint32_t)keep ? held - (uint32_t)keep : 0, may);
   if (row.thread == 0) a.n_evicted[lr] = (int32_t)n;
-  const bool same = a.tables_in == a.tables_out;
-  if (n == 0) {
-    if (!same) row.each([&](int32_t e, int32_t i, uint32_t) { if (e < row.E) out[e] = i; });
-    return;
-  }
-  // the n-th smallest key, and how many equal to it leave
-  uint32_t prefix = 0, mask = 0, equal = n;
-#pragma unroll 1
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = row.thread; i < 256; i += Row::kRowThreads) row.histogram[i] = 0;
-    row.sync();
-    row.each([&](int32_t, int32_t, uint32_t k) { if (k != kStays && (k & mask) == prefix) atomicAdd(&row.histogram[k >> shift & 255], 1u); });
-    row.sync();
-    // every wave finds the byte by itself: four bins a lane
-    const int lane = row.thread & 63;
-    const uint4 h = *(const uint4*)&row.histogram[4 * lane];
-    const uint32_t four = h.x + h.y + h.z + h.w;
-    uint32_t upto = four;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t y = __shfl_up(upto, d);
-      if (lane >= d) upto += y;
-    }
-    const int owner = __builtin_ctzll(__ballot(upto >= equal));
-    uint32_t before = upto - four, byte = 4 * lane;
-    if (before + h.x < equal) {
-      before += h.x, ++byte;
-      if (before + h.y < equal) {
-        before += h.y, ++byte;
-        if (before + h.z < equal) before += h.z, ++byte;
+  // keys below the border leave, and those that equal it at the entries before `place`
+  uint32_t border = 0, place = 0;
+  if (n) {
+    if constexpr (ITEMS) {
+      bool exact;
+      border = row.border(32, n, exact, [](int32_t, uint32_t k, uint32_t mid) { return k < mid; });
+      if (!exact) {
+        const uint32_t left = n - row.count([&](int32_t, uint32_t k) { return k < border; });
+        place = row.border(32 - __builtin_clz((uint32_t)row.E), left, exact, [&](int32_t e, uint32_t k, uint32_t mid) { return k == border && (uint32_t)e < mid; });
       }
-    }
-    equal -= __builtin_amdgcn_readlane(before, owner);
-    prefix |= (uint32_t)__builtin_amdgcn_readlane(byte, owner) << shift;
-    mask |= 255u << shift;
-    row.sync();
-  }
-  uint32_t taken = 0;  // of those equal to the key, in the entries before
-  row.each([&](int32_t e, int32_t i, uint32_t k) {
-    const bool is = k == prefix;
-    const uint64_t b = __ballot(is);
-    uint32_t rank = taken + __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0));
-    if constexpr (WAVES > 1) {
-      if ((row.thread & 63) == 0) row.scratch[row.thread >> 6] = __popcll(b);
-      __syncthreads();
-      uint32_t all = 0;
-      for (int v = 0; v < WAVES; ++v) {
-        const uint32_t c = row.scratch[v];
-        if (v < (row.thread >> 6)) rank += c;
-        all += c;
-      }
-      __syncthreads();
-      taken += all;
     } else {
-      taken += __popcll(b);
+      uint32_t equal;
+      border = row.nth(n, equal);
+      bool exact;
+      place = row.border(32 - __builtin_clz((uint32_t)row.E), equal, exact, [&](int32_t e, uint32_t k, uint32_t mid) { return k == border && (uint32_t)e < mid; });
     }
-    const bool leaves = k < prefix || (is && rank < equal);
+  }
+  const bool same = a.tables_in == a.tables_out;
+  if (n == 0 && same) return;
+  row.each([&](int32_t e, uint32_t k) {
+    const bool leaves = k < border || (k == border && (uint32_t)e < place);
+    if (e >= row.E || (same && !leaves)) return;
+    const int32_t i = row.in[e];
     if (leaves) atomicAdd(&a.refcount[l * a.NB + i], -1);
-    if (e < row.E && (leaves || !same)) out[e] = leaves ? -1 : i;
+    out[e] = leaves ? -1 : i;
   });
 }
 
@@ -259,19 +285,26 @@ extern "C" rc_status rc_kv_evict(int32_t n_layers, const int32_t* tables_in, int
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (NB > 0 && (!refcount_in || !refcount_out)) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
   if (R > 0 && (!ctx_len || !keep || !n_evicted || (E > 0 && (!tables_in || !tables_out || !weights)))) return fail(RC_ERR_INVALID_ARG, "%s: NULL pointer", who);
-  if (NB > 0 && refcount_in != refcount_out) {
-    const int64_t n = (int64_t)n_layers * NB, wgs = (n + kKvThreads - 1) / kKvThreads;
-    copy_counts_kernel<<<dim3((unsigned)(wgs < 4096 ? wgs : 4096)), kKvThreads, 0, st>>>(refcount_in, refcount_out, n);
+  const int64_t rows = (int64_t)n_layers * R, counts = (int64_t)n_layers * NB;
+  const bool small = E <= kSmallRow, copy = counts > 0 && refcount_in != refcount_out;
+  // a step of few short tables: one workgroup, one launch
+  const bool one = small && rows > 0 && rows <= 4 && counts <= 4096;
+  if (copy && !one) {
+    const int64_t wgs = (counts + kKvThreads - 1) / kKvThreads;
+    copy_counts_kernel<<<dim3((unsigned)(wgs < 4096 ? wgs : 4096)), kKvThreads, 0, st>>>(refcount_in, refcount_out, counts);
   }
   if (R > 0) {
-    const EvictArgs a = {tables_in, tables_out, n_layers, R, E, NB, block_tokens, ctx_len, keep, weights, n_first, n_last, refcount_out, n_evicted};
-    const int64_t rows = (int64_t)n_layers * R;
-    if (E <= 1024)
-      kv_evict_kernel<1, 16><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(a);
-    else if (E <= 16384)
-      kv_evict_kernel<16, 16><<<dim3((unsigned)rows), 1024, 0, st>>>(a);
+    const EvictArgs a = {tables_in, tables_out, n_layers, R, E, NB, block_tokens, ctx_len, keep, weights, n_first, n_last, copy && one ? refcount_in : nullptr,
+                         refcount_out, n_evicted};
+    const dim3 grid((unsigned)(small ? (rows + 3) / 4 : rows));
+    if (small)
+      kv_evict_kernel<1, kSmallRow / 64><<<grid, 256, 0, st>>>(a);
+    else if (E <= 16 * 1024)
+      kv_evict_kernel<16, 16><<<grid, 1024, 0, st>>>(a);
+    else if (E <= 32 * 1024)
+      kv_evict_kernel<16, 32><<<grid, 1024, 0, st>>>(a);
     else
-      kv_evict_kernel<16, 0><<<dim3((unsigned)rows), 1024, 0, st>>>(a);
+      kv_evict_kernel<16, 0><<<grid, 1024, 0, st>>>(a);
   }
   return check_launch(who);
 }

@@ -672,43 +672,46 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
   const KvAttendArgs& a = g.a;
   const int lane = threadIdx.x & 63, quarter = lane >> 4, col = lane & 15, chunks = (g.tiles + kWeighTiles - 1) / kWeighTiles;
-  const int64_t tasks = a.s.L * a.s.R * a.s.H * chunks * (int64_t)g.shares;
+  const int64_t heads = a.s.L * a.s.R * a.s.H, tasks = heads * chunks * g.shares;
   for (int64_t task = (int64_t)blockIdx.x * kWaves + uniform((int)(threadIdx.x >> 6)); task < tasks; task += (int64_t)gridDim.x * kWaves) {
-    // shares beside each other: they read the same K
-    int64_t i = task / g.shares;
-    const int share = (int)(task - i * g.shares), chunk = (int)(i % chunks);
-    i /= chunks;
+    // shares beside each other: they read the same K; the first chunks, which most rows see, before the later ones
+    const int64_t i = task / g.shares;
+    const int share = (int)(task - i * g.shares), chunk = (int)(i / heads);
+    int64_t at = i - chunk * heads;
     Walk w;
-    w.h = (int)(i % a.s.H);
-    i /= a.s.H;
-    w.r = (int)(i % a.s.R), w.l = (int)(i / a.s.R), w.t = 0;
+    w.h = (int)(at % a.s.H);
+    at /= a.s.H;
+    w.r = (int)(at % a.s.R), w.l = (int)(at / a.s.R), w.t = 0;
     w.q = request(a, w.r);
     const int pos0 = chunk * kWeighTiles * 16, first = w.q.ctx - w.q.len;
     if (w.q.rows == 0) continue;
     // the rows that see any of these tokens
     const int last = first + (w.q.rows - 1) / a.s.g;
     if (attend_high(a.s, last) <= pos0 || attend_low(a.s, first) >= pos0 + kWeighTiles * 16) continue;
+    // the row tiles that see any of these tokens, and the task's share of them
+    const int g_ = a.s.g, end = pos0 + kWeighTiles * 16;
+    const int64_t beyond = a.s.window ? ((int64_t)end + a.s.window - 1 - first) * g_ : w.q.rows;
+    const int t0 = pos0 > first ? (int)(((int64_t)pos0 - first) * g_ / 16) : 0, t1 = (int)((min(beyond, (int64_t)w.q.rows) + 15) / 16);
+    const int64_t all = max(t1 - t0, 0);
+    const int from = t0 + (int)(all * share / g.shares), to = t0 + (int)(all * (share + 1) / g.shares);
     const int32_t* table = a.tables + ((int64_t)w.l * a.s.R + w.r) * a.s.E;
     const char* head_k = a.k + (int64_t)w.l * a.layer_stride_b + w.h * 256 + (lane & 15) * a.token_b + quarter * 16;
     u32x4 k[kWeighTiles][4];
     int there = 0;
-    const int ids = load_id(a, table, chunk * kWeighTiles + (lane & 7), true);
+    const int ids = from < to ? load_id(a, table, chunk * kWeighTiles + (lane & (kWeighTiles - 1)), true) : -1;
+    if (from < to) {
 #pragma unroll
-    for (int j = 0; j < kWeighTiles; ++j) {
-      bool is;
-      const uint64_t at = tile_offset(a, __builtin_amdgcn_readlane(ids, j), j & 1, is);
-      there |= (int)is << j;
+      for (int j = 0; j < kWeighTiles; ++j) {
+        bool is;
+        const uint64_t at = tile_offset(a, __builtin_amdgcn_readlane(ids, j), j & 1, is);
+        there |= (int)is << j;
 #pragma unroll
-      for (int d = 0; d < 4; ++d) k[j][d] = *(const u32x4*)(head_k + at + d * 64);
+        for (int d = 0; d < 4; ++d) k[j][d] = *(const u32x4*)(head_k + at + d * 64);
+      }
     }
     float sum[kWeighTiles];
 #pragma unroll
     for (int j = 0; j < kWeighTiles; ++j) sum[j] = 0.f;
-    // the row tiles that see any of these tokens, and the task's share of them
-    const int g_ = a.s.g, end = pos0 + kWeighTiles * 16;
-    const int64_t beyond = a.s.window ? ((int64_t)end + a.s.window - 1 - first) * g_ : w.q.rows;
-    const int t0 = pos0 > first ? (int)((int64_t)(pos0 - first) * g_ / 16) : 0, t1 = (int)((min(beyond, (int64_t)w.q.rows) + 15) / 16);
-    const int from = t0 + (int)((int64_t)(t1 - t0) * share / g.shares), to = t0 + (int)((int64_t)(t1 - t0) * (share + 1) / g.shares);
     struct Rows {
       u32x4 q[4];
       float2 end;
@@ -727,34 +730,45 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
       // a row that is not there, or that sees nothing: no weight, and a reference that no score comes near
       const bool none = t * 16 + col >= w.q.rows || x.end.y == 0.f;
       const float f = none ? 0.f : 1.f / x.end.y, ref = none ? -kNothing : x.end.x;
-      const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) < end || there != 255;
+      const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) < end || there != (1 << kWeighTiles) - 1;
       const int low = attend_low(a.s, x.pos);
       const uint32_t span = max(attend_high(a.s, x.pos) - low, 0);
       const bool coarse = uniform(__any(f != 0.f && fabsf(ref) > kCoarse));
+      // four tiles at a time: a product waits for the one before it of the same tile
 #pragma unroll
-      for (int j = 0; j < kWeighTiles; ++j) {
-        f32x4 s = {0, 0, 0, 0};
+      for (int j0 = 0; j0 < kWeighTiles; j0 += 4) {
+        f32x4 s[4];
 #pragma unroll
-        for (int d = 0; d < 4; ++d) s = mfma<BF16>(k[j][d], x.q[d], s);
-        if (ends) {
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const bool is = (uint32_t)(pos0 + 16 * j + 4 * quarter + r - low) < (there >> j & 1 ? span : 0u);
-            s[r] = is ? s[r] : -__builtin_inff();
+          for (int j = 0; j < 4; ++j) s[j] = mfma<BF16>(k[j0 + j][d], x.q[d], d ? s[j] : f32x4{0, 0, 0, 0});
+        __builtin_amdgcn_sched_barrier(0);
+        if (__builtin_expect(ends, 0)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int j = j0 + (i >> 2);
+            const bool is = (uint32_t)(pos0 + 16 * j + 4 * quarter + (i & 3) - low) < (there >> j & 1 ? span : 0u);
+            s[i >> 2][i & 3] = is ? s[i >> 2][i & 3] : -__builtin_inff();
           }
         }
-        float p[4];
+        if (__builtin_expect(coarse, 0)) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float e = fmaf(s[r], a.c, -ref);
-          if (__builtin_expect(coarse, 0)) {
+          for (int i = 0; i < 16; ++i) {
 #pragma clang fp contract(off)
-            const float z = s[r] * a.c, d = z - ref;
-            e = fabsf(ref) > kCoarse ? d : e;
+            const float z = s[i >> 2][i & 3] * a.c, d = z - ref;
+            s[i >> 2][i & 3] = fabsf(ref) > kCoarse ? d : fmaf(s[i >> 2][i & 3], a.c, -ref);
           }
-          p[r] = __builtin_amdgcn_exp2f(e);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i >> 2][i & 3] = fmaf(s[i >> 2][i & 3], a.c, -ref);
         }
-        sum[j] = fmaf((p[0] + p[1]) + (p[2] + p[3]), f, sum[j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float p[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[j][r]);
+          sum[j0 + j] = fmaf((p[0] + p[1]) + (p[2] + p[3]), f, sum[j0 + j]);
+        }
       }
     };
     // the next rows are on their way beside the products of these

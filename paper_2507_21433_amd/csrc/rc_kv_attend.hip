@@ -231,18 +231,18 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
     if (more) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) load_k<STREAM>(x[j], head_k + at[j], lanes);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], head_v + at[j], lanes);
-      // (these loads and those at the loop's end would become one at its beginning, were there nothing different behind them)
-      asm volatile("; the first run is on its way" ::: "memory");
     }
-    // The next run's K is on its way from where this one's is used up, and V likewise.  The loads are never left out (behind the
+    // A run's V is on its way from where its K is used, the next one's K from where this one's is used up: more at a time (V behind the last run's
+    // products) is slower, 390 us for 381 (64 requests of up to 12400 tokens) and 97 for 87 (24 rows).  The loads are never left out (behind the
     // last run that one is loaded again): where a branch goes round them, a wait for some of the loads becomes a wait for all.
 #pragma unroll 1
     while (more) {
       const int pair = part.pa + wave + kWaves * n, pos = pair * kPairTokens;
       const uint64_t here[2] = {at[0], at[1]};
       there[0] = there_next[0], there[1] = there_next[1];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], head_v + here[j], lanes);
+      __builtin_amdgcn_sched_barrier(0);
       f32x4 s[RT][2];
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -319,10 +319,6 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
       chunks(std::integral_constant<int, 1>{});
       chunks(std::integral_constant<int, 2>{});
       chunks(std::integral_constant<int, 3>{});
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) load_v<STREAM>(x[j], head_v + at[j], lanes);
-      asm volatile("; the next run is on its way" ::: "memory");
     }
 
     // the four waves' sums, under the largest of their references

@@ -82,7 +82,9 @@ struct EvictRow {
   int32_t E, used, thread;
   uint32_t* lds;  // 2 * WAVES sums, and 256 more without registers
   int turn;
+  static constexpr bool kIds = ITEMS && ITEMS <= 16;  // ids are held as well, else read again where they are written
   uint32_t key[ITEMS ? ITEMS : 1];
+  int32_t id[kIds ? ITEMS : 1];
 
   __device__ __forceinline__ bool held(int32_t i, int32_t e) const { return e < used && i >= 0 && i < a.NB; }
   __device__ __forceinline__ uint32_t make_key(int32_t i, int32_t e) const {
@@ -102,14 +104,21 @@ struct EvictRow {
   // f(entry, key) of every entry of the thread; the same number of turns for all lanes of the row.
   template <class F>
   __device__ __forceinline__ void each(F f) {
+    each_id([&](int32_t e, uint32_t k, auto) { f(e, k); });
+  }
+  // ... and its id, asked for as a function
+  template <class F>
+  __device__ __forceinline__ void each_id(F f) {
     if constexpr (ITEMS) {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i)
-        if (i * kRowThreads < E) f(i * kRowThreads + thread, key[i]);
+      for (int i = 0; i < ITEMS; ++i) {
+        const int32_t e = i * kRowThreads + thread;
+        if (i * kRowThreads < E) f(e, key[i], [&] { return kIds ? id[kIds ? i : 0] : in[e]; });
+      }
     } else {
       for (int32_t base = 0; base < E; base += kRowThreads) {
         const int32_t e = base + thread;
-        f(e, make_key(e < E ? in[e] : -1, e));
+        f(e, make_key(e < E ? in[e] : -1, e), [&] { return in[e]; });
       }
     }
   }
@@ -184,7 +193,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void kv_evict_kernel
   const int64_t lr = (int64_t)blockIdx.x * kRows + in_block;
   if (lr >= a.L * a.R) return;
   const int64_t l = lr / a.R, r = lr - l * a.R;
-  Row row{a, a.tables_in + lr * a.E, a.weights + lr * a.E, (int32_t)a.E, 0, (int)(WAVES == 1 ? threadIdx.x & 63 : threadIdx.x), lds, 0, {}};
+  Row row{a, a.tables_in + lr * a.E, a.weights + lr * a.E, (int32_t)a.E, 0, (int)(WAVES == 1 ? threadIdx.x & 63 : threadIdx.x), lds, 0, {}, {}};
   int32_t* out = a.tables_out + lr * a.E;
   const int32_t ctx = a.ctx_len[r], keep = max(a.keep[r], 0);
   const int64_t blocks = ctx > 0 ? ((int64_t)ctx + a.T - 1) / a.T : 0;
@@ -201,6 +210,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void kv_evict_kernel
     for (int i = 0; i < ITEMS; ++i) {
       const int32_t e = i * Row::kRowThreads + row.thread;
       row.key[i] = row.make_key(id[i], e);
+      if constexpr (Row::kIds) row.id[i] = id[i];
       held += __popcll(__ballot(row.held(id[i], e)));
     }
     held = row.sum_waves(held);
@@ -229,10 +239,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void kv_evict_kernel
   }
   const bool same = a.tables_in == a.tables_out;
   if (n == 0 && same) return;
-  row.each([&](int32_t e, uint32_t k) {
+  row.each_id([&](int32_t e, uint32_t k, auto id) {
     const bool leaves = k < border || (k == border && (uint32_t)e < place);
     if (e >= row.E || (same && !leaves)) return;
-    const int32_t i = row.in[e];
+    const int32_t i = id();
     if (leaves) atomicAdd(&a.refcount[l * a.NB + i], -1);
     out[e] = leaves ? -1 : i;
   });

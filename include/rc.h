@@ -511,7 +511,7 @@ rc_status rc_cache_attend(const rc_cache_desc* desc, const void* cache, const in
 rc_status rc_kv_write(const rc_kv_desc* desc, int64_t n_blocks, const void* k_new, const void* v_new, int64_t n_tokens,
                       int64_t token_stride, int64_t new_layer_stride, const int32_t* slots, void* k, void* v, void* hip_stream);
 
-/* Bytes of DEVICE workspace rc_kv_attend needs, with weights_out if `weigh` (0 on bad arguments; without weights up to 69 MB, with them also
+/* Bytes of DEVICE workspace rc_kv_attend needs, with weights_out if `weigh` (0 on bad arguments; without weights up to 103 MB, with them also
  * 8 bytes per query token and head, and per layer, request and KV head half a byte per table position and row (query tokens times heads of a KV head)
  * of the largest step of at most 32 rows, or where that is more 8 bytes per position and layer, request and KV head).  It depends on the arguments only
  * and never falls as R, E, n_q, max_q or the layers grow. */
@@ -547,8 +547,9 @@ size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_blocks, int
  *   workspace       DEVICE, 16-byte aligned, rc_kv_attend_workspace_size() bytes.  Contents are scratch.  Calls that share it
  *                   must not overlap.
  * Sums and softmax statistics are fp32; for the matrix cores a probability is the sum of two numbers of the 16-bit type where max_q * g is
- * at most 16, else one.  No atomics: the same bits on every run.  Sums of finite values neither overflow nor lose their values; a query that sees an
- * infinity or a NaN in V has infinities or NaNs in these dims, one that does not see them is as if they were not there.
+ * at most 16, else one.  No atomics: the same bits on every run.  Sums of finite values neither overflow nor lose their values (but weights are not
+ * defined where scale * log2(e) * q.k is beyond 2^20, so that fp32 numbers there are whole ones, and bf16 values are beyond 2^64 at the same time); a query
+ * that sees an infinity or a NaN in V has infinities or NaNs in these dims, one that does not see them is as if they were not there.
  */
 rc_status rc_kv_attend(const rc_kv_desc* desc, int64_t n_blocks, const void* k, const void* v, const int32_t* tables, int64_t R, int64_t E,
                        const int32_t* ctx_len, const int32_t* q_start, const void* q, int64_t n_q, int32_t n_heads,

@@ -11,7 +11,8 @@ constexpr int kKvThreads = 256;
 
 // ---- rc_kv_write
 
-// A copy, bound by memory: a thread moves 16 bytes of K and of V at a time, four of each, neighbouring threads neighbouring ones.
+// A copy, bound by memory: a thread moves 16 bytes of K and of V at a time, four of each, neighbouring threads neighbouring ones.  64 layers of 2.1k tokens
+// 1.12 GB in 204 us (5.5 TB/s; a copy of 4 GB runs at 4.6); the smallest calls are a launch, 3 us.
 struct KvWriteArgs {
   const char *k_new, *v_new;
   const int32_t* slots;
@@ -73,6 +74,10 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // lie before a place of the table: both are found bit by bit from the top, with a count of the entries below at every bit.  Keys lie in registers (entry
 // i * threads + thread at place i), so that a count is a compare and a ballot for each; a row that they do not hold is counted by a histogram of
 // each byte in turn, for which it is read again.
+//
+// 64 layers of 64 requests of up to 775 entries, 700 kept at most: 29 us and 5 for the copy of the reference counts; 11 of these are the 1M decrements, 11 the tables and
+// weights going in and out, the borders the rest (a histogram by bytes for these as well: the same).  24 tables of 16384 entries cut down to a quarter: 46 us, 24 workgroups'
+// work, 19 for the decrements (with histograms 62).
 template <int WAVES, int ITEMS>  // ITEMS: entries of a thread held in registers, 0: none
 struct EvictRow {
   static constexpr int kRowThreads = 64 * WAVES;

@@ -4,8 +4,8 @@
 // Scores are taken as S^T = K Q^T and outputs as O^T = V^T P^T on 16x16x32 matrix instructions: a row (a query token and head) is a
 // column of both, so that its scores, its probabilities and its sums lie in the same four lanes and the probabilities go from
 // one product into the next as they are.  A token's head is 256 bytes in a row of memory.  K's operand (a lane: 8 dims of a token) is what a
-// load of 16 bytes brings; V's (a lane: 8 tokens of a dim) are eight such loads, of eight tokens, whose halves are paired by one byte permute
-// for each two values: no value moves between lanes.
+// load of 16 bytes brings.  V's (a lane: 8 tokens of a dim) are, with few rows, eight such loads, of eight tokens, whose halves are paired by one byte
+// permute for each two values, so that no value moves between lanes; with many rows V lies in LDS token by token and is read transposed.
 #include <hip/hip_runtime.h>
 
 #include "rc_attend.hpp"
@@ -158,6 +158,10 @@ struct RowsLds {
   float o[kWaves][16][132];
 };
 
+// What bounds it is memory: 64 requests of up to 12400 tokens 2.18 GB in 377 us at the card's steady speed (5.8 TB/s; a read of 4 GB runs at 5.9), one of
+// 262143 tokens 1.07 GB in 194 (5.5).  Two waves a SIMD: for three (168 registers, some of a run's values in memory) 470 us and 247.  Calls of few rows and short contexts
+// are bound by what comes one after the other: 300 tokens 9.5 us, a launch, the lengths, the block ids, three runs of 32 tokens a wave, the joining of four
+// waves.  With weights a wave leaves the sums of the two tiles of a run and its reference for every row, 16 bytes beside the run's 16384.
 template <bool BF16, int RT, bool STREAM, bool WEIGH>
 __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
   // Probabilities as sums of two 16-bit numbers: with one row tile the matrix cores have the time, and the only rounding
@@ -379,6 +383,13 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
 // memory, three runs ahead of the one that is computed.  K comes in operand order: a lane asks for the 16 bytes that it will hold.
 // V comes token by token, and reads that transpose give a lane four tokens of a dim; the 16-byte units of a token's 256 are exchanged by its
 // number (unit u lies at u ^ token % 4), so that the sixteen lanes of such a read, four tokens and four units of each, find different banks.
+//
+// A run of a wave with 48 rows is 48 matrix instructions (768 cycles), some 110 other vector instructions, 24 of them exponentials, and 16 KB of LDS.  A chunk of
+// 1024 query tokens over 8192: 220 GFLOP in 242 us at the card's steady speed (910 TFLOP/s; a library product of 8192^3 runs at 1155) and 16 for the parts of cut items; a
+// SIMD's matrix unit is busy 39 % of the time.  Two waves a SIMD, each a chain of reads, products, exponentials and products, do not cover each other's waits:
+// workgroups of equal work end between 190 and 286 us.  What was tried against that: wave tiles of 32 rows 280 us, steps of 64 tokens to a barrier 258, products
+// woven between exponentials 260, K and V through registers 293, two groups of four waves that take turns at the matrix cores with a barrier at each turn 320 to 385.
+// Without the loads it takes 237, without the exponentials 223.
 
 constexpr int kRuns = 4;  // buffers
 
@@ -661,7 +672,9 @@ struct WeighArgs {
 };
 
 // Many rows: the probabilities are taken once more, from K, Q and the rows' final references and sums: a wave holds the K of 128 tokens and goes through a
-// share of the request's rows.  (Kept from the first time they would be a number for each row and 16 tokens: 10 GB for a prompt of 32k tokens and 40 heads.)
+// share of the rows that see them.  (Kept from the first time they would be a number for each row and 16 tokens: 10 GB for a prompt of 32k tokens and 40 heads.)
+// Prompts of 2500 tokens and 32 heads: 51 GFLOP in 112 us, bound by the way of Q from the caches (64 tokens a wave 142 us, 32 and 64 shares of the rows
+// instead of 16 122 and 149; with the rows read when they are needed 228, with one tile's products after another's 147).
 constexpr int kWeighTiles = 8;
 
 template <bool BF16>
@@ -836,11 +849,19 @@ __global__ __launch_bounds__(kThreads) void weigh_entries_kernel(WeighArgs g) {
 
 // ---- The call.
 
+// Kernels by the rows of a request and KV head (query tokens times heads of a KV head): tiles of 16 and 32 rows, where every wave of a workgroup has all rows
+// and a quarter of the tokens, and of 64, 128 and 192, where every wave has a quarter of the rows.  Larger tiles read the blocks less often and cost
+// more to begin and end.  us with tiles of 64 / 128 / 192 rows, by the number of tiles of 128 and of steps of 64 tokens that a table has: 8 x 63 23 / 28 / 33,
+// 64 x 16 28 / 37 / 42, 24 x 63 33 / 33 / 39, 32 x 63 32 / 36 / 43, 64 x 63 50 / 52 / 62, 256 x 16 35 / 42 / 43; 320 x 16 53 / 39 / 43,
+// 512 x 8 39 / 34 / 39, 24 x 250 62 / 58 / 70, 128 x 63 71 / 67 / 82, 64 x 250 121 / 105 / 108, 2560 x 5 103 / 82 / 86; 640 x 63 - / 194 / 200,
+// 320 x 125 - / 195 / 193, 260 x 250 - / 361 / 336, 1280 x 125 - / 671 / 632.  An item of many rows costs three steps besides its own (1, 3 and 5 tried:
+// prompts of 2500 tokens 181, 152 and 154 us, a chunk of 1024 285 to 289).
 inline AttendKernel kv_kernel(int64_t rows, double pairs, int64_t steps) {
   if (rows <= 16) return {16, 128, 768, 4, 2};
   if (rows <= 32) return {32, 128, 512, 4, 1};
-  const double tiles = pairs * (double)((rows + 127) / 128);
-  if (rows <= 64 || (tiles <= 128 && tiles * (double)steps <= 8192)) return {64, 64, 512, 8, 1};
+  const double tiles = pairs * (double)((rows + 127) / 128), work = tiles * (double)steps;
+  if (rows <= 64 || (tiles <= 256 && work <= 4096)) return {64, 64, 512, 8, 1};
+  if (work <= 49152) return {128, 64, 512, 8, 3};
   return {192, 64, 512, 8, 3};
 }
 
@@ -907,6 +928,8 @@ void kv_launch(const WeighArgs& g, hipStream_t st) {
     stream ? kv_rows_launch<BF16, true, false>(a, st) : kv_rows_launch<BF16, false, false>(a, st);
   else if (a.s.rows == 64)
     kv_many_kernel<BF16, 1><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
+  else if (a.s.rows == 128)
+    kv_many_kernel<BF16, 2><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
   else
     kv_many_kernel<BF16, 3><<<dim3(a.s.wgs), kThreads, 0, st>>>(a);
   if (a.borders) {
@@ -948,7 +971,7 @@ extern "C" size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_
     if ((double)s.L * n_q * n_heads > 1e15) return 0;
     const int64_t runs = runs_of(s), few = max_q < kFewRows / s.g ? max_q : kFewRows / s.g;
     const int64_t a = few_room(s.L, R, s.H, runs, few * s.g).bytes(), b = kMostShares * many_room(s.L, R, s.H, runs, 1).bytes();
-    n = (size_t)up16((int64_t)n) + (size_t)up16(s.L * n_q * n_heads * 8) + (size_t)(max_q * s.g > kFewRows && b > a ? b : a);
+    n = (size_t)up16((int64_t)n) + (size_t)up16(s.L * n_q * n_heads * 8) + (size_t)(max_q > kFewRows / s.g && b > a ? b : a);
   }
   return n;
 }

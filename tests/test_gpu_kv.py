@@ -362,8 +362,8 @@ def test_blocks_of_none(dtype):
     assert not r["out"].any() and (r["lse"] == -math.inf).all() and r["weights"].numel() == 0
 
 
-# query tokens, query heads of a KV head, entries of a table: tiles of 16, 32, 64 and 128 rows, items that are cut and whole ones
-KERNELS = [(1, 4, None), (1, 4, WIDE), (5, 4, None), (5, 4, WIDE), (12, 4, None), (12, 4, WIDE), (40, 4, 20 * WIDE)]
+# query tokens, query heads of a KV head, entries of a table: tiles of 16, 32, 64, 128 and 192 rows, items that are cut and whole ones
+KERNELS = [(1, 4, None), (1, 4, WIDE), (5, 4, None), (5, 4, WIDE), (12, 4, None), (12, 4, WIDE), (40, 4, 5000), (40, 4, 20 * WIDE)]
 
 
 @pytest.mark.parametrize("m,g,E", KERNELS + [(20, 5, 20 * WIDE), (1, 5, None), (1, 3, WIDE), (7, 7, None)])
@@ -676,3 +676,19 @@ def test_another_stream():
         r = p.run(**args)
     torch.cuda.current_stream().wait_stream(other)
     assert all(torch.equal(r[x], want[x]) for x in r)
+
+
+@pytest.mark.parametrize("g,m", [(33, 1), (64, 2), (200, 1), (1024, 1)])
+def test_many_heads_of_a_kv_head(g, m):
+    p = Problem([(300, m), (45, m), (0, m)], 1, g, 16, HALF, gathered=True)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("R,m,E", [(1, 700, 60), (3, 300, 60), (70, 40, 30), (130, 30, 30), (2, 900, 5000)])
+def test_row_tiles_of_few_and_many_requests(R, m, E):
+    """Lanes that count the tiles of one request together, or of one request each; stretches that begin in any tile."""
+    gn = gen(R)
+    requests = [(int(torch.randint(m, 480, (1,), generator=gn)) if E < 1000 and m < 480 else m + 60, int(torch.randint(1, m + 1, (1,), generator=gn))) for _ in range(R)]
+    requests[R // 2] = (max(m, 470), m)
+    p = Problem(requests, 2, 3, 16, BF, E=E, gathered=True)
+    p.check(p.run())

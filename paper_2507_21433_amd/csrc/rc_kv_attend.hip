@@ -158,15 +158,14 @@ struct RowsLds {
   float o[kWaves][16][132];
 };
 
-// What bounds it is memory: 64 requests of up to 12400 tokens 2.18 GB in 377 us at the card's steady speed (5.8 TB/s; a read of 4 GB runs at 5.9), one of
+// What bounds it is memory: 64 requests of up to 12400 tokens 2.18 GB in 381 us (5.7 TB/s; a read of 4 GB runs at 5.9), one of
 // 262143 tokens 1.07 GB in 194 (5.5).  Two waves a SIMD: for three (168 registers, some of a run's values in memory) 470 us and 247.  Calls of few rows and short contexts
 // are bound by what comes one after the other: 300 tokens 9.5 us, a launch, the lengths, the block ids, three runs of 32 tokens a wave, the joining of four
 // waves.  With weights a wave leaves the sums of the two tiles of a run and its reference for every row, 16 bytes beside the run's 16384.
 template <bool BF16, int RT, bool STREAM, bool WEIGH>
 __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
-  // Probabilities as sums of two 16-bit numbers: with one row tile the matrix cores have the time, and the only rounding
-  // that counts is that of the output; with two tiles they are rounded once, which in the output is as much as its own rounding.
-  constexpr bool kTwo = RT == 1;
+  // Probabilities are sums of two 16-bit numbers: the matrix cores have the time (two row tiles 83 us for 91 with one number, which the registers that the
+  // compiler then finds explain), and the only rounding that counts is that of the output.
   __shared__ RowsLds<RT> lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
@@ -298,9 +297,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t two = kTwo ? cut2<BF16>(p[2 * j], p[2 * j + 1]) : pack2<BF16>(p[2 * j], p[2 * j + 1]);
+          const uint32_t two = cut2<BF16>(p[2 * j], p[2 * j + 1]);
           hi[t][j] = two;
-          if (kTwo) lo[t][j] = cut2<BF16>(p[2 * j] - low16<BF16>(two), p[2 * j + 1] - high16<BF16>(two));
+          lo[t][j] = cut2<BF16>(p[2 * j] - low16<BF16>(two), p[2 * j + 1] - high16<BF16>(two));
         }
       }
       const auto chunks = [&](auto b) {
@@ -313,10 +312,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
         for (int t = 0; t < RT; ++t) {
           o[t][2 * B] = mfma<BF16>(even, hi[t], o[t][2 * B]);
           o[t][2 * B + 1] = mfma<BF16>(odd, hi[t], o[t][2 * B + 1]);
-          if (kTwo) {
-            o[t][2 * B] = mfma<BF16>(even, lo[t], o[t][2 * B]);
-            o[t][2 * B + 1] = mfma<BF16>(odd, lo[t], o[t][2 * B + 1]);
-          }
+          o[t][2 * B] = mfma<BF16>(even, lo[t], o[t][2 * B]);
+          o[t][2 * B + 1] = mfma<BF16>(odd, lo[t], o[t][2 * B + 1]);
         }
       };
       chunks(std::integral_constant<int, 0>{});
@@ -385,11 +382,11 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
 // number (unit u lies at u ^ token % 4), so that the sixteen lanes of such a read, four tokens and four units of each, find different banks.
 //
 // A run of a wave with 48 rows is 48 matrix instructions (768 cycles), some 110 other vector instructions, 24 of them exponentials, and 16 KB of LDS.  A chunk of
-// 1024 query tokens over 8192: 220 GFLOP in 242 us at the card's steady speed (910 TFLOP/s; a library product of 8192^3 runs at 1155) and 16 for the parts of cut items; a
-// SIMD's matrix unit is busy 39 % of the time.  Two waves a SIMD, each a chain of reads, products, exponentials and products, do not cover each other's waits:
-// workgroups of equal work end between 190 and 286 us.  What was tried against that: wave tiles of 32 rows 280 us, steps of 64 tokens to a barrier 258, products
+// 1024 query tokens over 8192: 220 GFLOP in 237 us at the card's steady speed (930 TFLOP/s; a library product of 8192^3 runs at 1155) and 16 for the parts of cut items; a
+// SIMD's matrix unit is busy for 39 % of the time, its other vector instructions take 28 %, a compute unit's LDS 20 %.  Two waves a SIMD, each a chain of reads, products, exponentials and products, do not cover each other's waits:
+// workgroups of equal work end between 190 and 286 us.  What was tried against that (us before the card has reached its speed, 256 as it is): wave tiles of 32 rows 280 us, steps of 64 tokens to a barrier 258, products
 // woven between exponentials 260, K and V through registers 293, two groups of four waves that take turns at the matrix cores with a barrier at each turn 320 to 385.
-// Without the loads it takes 237, without the exponentials 223.
+// Without the loads it takes 8 % less, without the exponentials 14 %.
 
 constexpr int kRuns = 4;  // buffers
 
@@ -673,7 +670,7 @@ struct WeighArgs {
 
 // Many rows: the probabilities are taken once more, from K, Q and the rows' final references and sums: a wave holds the K of 128 tokens and goes through a
 // share of the rows that see them.  (Kept from the first time they would be a number for each row and 16 tokens: 10 GB for a prompt of 32k tokens and 40 heads.)
-// Prompts of 2500 tokens and 32 heads: 51 GFLOP in 112 us, bound by the way of Q from the caches (64 tokens a wave 142 us, 32 and 64 shares of the rows
+// Prompts of 2500 tokens and 32 heads: 51 GFLOP in 105 us, bound by the way of Q from the caches (117 us where 64 tokens a wave take 142, 32 and 64 shares of the rows
 // instead of 16 122 and 149; with the rows read when they are needed 228, with one tile's products after another's 147).
 constexpr int kWeighTiles = 8;
 

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2507_21433_amd import binding as rc
+from tests import cache_cancelling
 from tests import kv_reference as ref
 
 pytestmark = pytest.mark.gpu
@@ -115,7 +116,7 @@ class Problem:
         self.rewrite(k.to(dtype), v.to(dtype))
         self.q = randn((L, N, H * g, 128), gn, dtype).to(DEV)
         self.scale, self.window, self.max_q = 128 ** -0.5, 0, max(self.new)
-        self.many = self.max_q * g > 16      # probabilities rounded once
+        self.many = self.max_q * g > 32      # probabilities rounded once
         self.gathered = torch.rand((L, R, E), generator=gn).to(DEV) * 50 if gathered else None
 
     def rewrite(self, k=None, v=None):
@@ -267,6 +268,23 @@ def test_sharp_and_flat_softmax(scale, m):
     p = Problem([(900, m), (1100, m)], 1, 5, 16, HALF, E=None if scale < 1 else WIDE, strong=True)
     p.scale = scale
     p.check(p.run())
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("g,n,E", [(1, 40, None), (4, 64, None), (16, 128, WIDE), (17, 97, None), (25, 110, WIDE), (32, 128, None)])
+@pytest.mark.parametrize("weigh", [False, True])
+def test_few_rows_lose_nothing_of_their_probabilities(g, n, E, dtype, weigh):
+    """With up to 32 rows a probability is the sum of two 16-bit numbers: outputs that nearly cancel are as close as that makes them."""
+    say(g, n, E, dtype, weigh)
+    p = Problem([(n, 1)], 1, g, 16, dtype, E=E)
+    q, k, v = cache_cancelling.problem(g, n, dtype, gen(g))
+    p.rewrite(torch.nn.functional.pad(k[None, :, None, None], (0, 127)), v[None, :, None])
+    p.q = torch.nn.functional.pad(q[None, None, :, None], (0, 127)).to(DEV)
+    p.scale = 1.0
+    weights = cache_cancelling.weights(q, k)
+    off = (p.run(want_weights=weigh)["out"][0, 0].cpu().double() - weights @ v.double()).abs() / cache_cancelling.bound(weights, v.double(), dtype)
+    say("largest error in bounds:", off.max().item())
+    assert off.max() <= 1
 
 
 def test_scores_that_climb():

@@ -513,8 +513,8 @@ rc_status rc_kv_write(const rc_kv_desc* desc, int64_t n_blocks, const void* k_ne
 
 /* Bytes of DEVICE workspace rc_kv_attend needs, with weights_out if `weigh` (0 on bad arguments; without weights up to 103 MB, with them also
  * 8 bytes per query token and head, and per layer, request and KV head half a byte per table position and row (query tokens times heads of a KV head)
- * of the largest step of at most 32 rows, or where that is more 8 bytes per position and layer, request and KV head).  It depends on the arguments only
- * and never falls as R, E, n_q, max_q or the layers grow. */
+ * of the largest step of at most 32 rows, or where that is more a quarter of a byte per position and layer, request and KV head, or up to 256 KB).  It
+ * depends on the arguments only and never falls as R, E, n_q, max_q or the layers grow. */
 size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_blocks, int64_t R, int64_t E, int32_t n_heads, int64_t n_q,
                                    int64_t max_q, int32_t weigh);
 

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void kv_evict_kernel
     __threadfence();
     __syncthreads();
   }
-  const int64_t lr = (int64_t)blockIdx.x * kRows + in_block;
+  const int64_t lr = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + in_block;
   if (lr >= a.L * a.R) return;
   const int64_t l = lr / a.R, r = lr - l * a.R;
   Row row{a, a.tables_in + lr * a.E, a.weights + lr * a.E, (int32_t)a.E, 0, (int)(WAVES == 1 ? threadIdx.x & 63 : threadIdx.x), lds, 0, {}, {}};
@@ -311,7 +311,9 @@ extern "C" rc_status rc_kv_evict(int32_t n_layers, const int32_t* tables_in, int
   if (R > 0) {
     const EvictArgs a = {tables_in, tables_out, n_layers, R, E, NB, block_tokens, ctx_len, keep, weights, n_first, n_last, copy && one ? refcount_in : nullptr,
                          refcount_out, n_evicted};
-    const dim3 grid((unsigned)(small ? (rows + 3) / 4 : rows));
+    // (a launch has fewer than 2^32 threads in x)
+    const int64_t wgs = small ? (rows + 3) / 4 : rows, x = wgs < (1 << 20) ? wgs : (1 << 20);
+    const dim3 grid((unsigned)x, (unsigned)((wgs + x - 1) / x));
     if (small)
       kv_evict_kernel<1, kSmallRow / 64><<<grid, 256, 0, st>>>(a);
     else if (E <= 16 * 1024)

@@ -164,8 +164,8 @@ struct RowsLds {
 // waves.  With weights a wave leaves the sums of the two tiles of a run and its reference for every row, 16 bytes beside the run's 16384.
 template <bool BF16, int RT, bool STREAM, bool WEIGH>
 __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
-  // Probabilities are sums of two 16-bit numbers: the matrix cores have the time (two row tiles 83 us for 91 with one number, which the registers that the
-  // compiler then finds explain), and the only rounding that counts is that of the output.
+  // Probabilities are sums of two 16-bit numbers: the matrix cores have the time (24 rows over 305 MB: 72 us, and 84 with
+  // one number, where the compiler spills 328 B a thread instead of 184), and the only rounding that counts is that of the output.
   __shared__ RowsLds<RT> lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
@@ -689,14 +689,14 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
     at /= a.s.H;
     w.r = (int)(at % a.s.R), w.l = (int)(at / a.s.R), w.t = 0;
     w.q = request(a, w.r);
-    const int pos0 = chunk * kWeighTiles * 16, first = w.q.ctx - w.q.len;
+    const int pos0 = chunk * kWeighTiles * 16, pos1 = pos0 + (kWeighTiles * 16 - 1), first = w.q.ctx - w.q.len;  // (pos1 + 1 may be 2^31)
     if (w.q.rows == 0) continue;
     // the rows that see any of these tokens
     const int last = first + (w.q.rows - 1) / a.s.g;
-    if (attend_high(a.s, last) <= pos0 || attend_low(a.s, first) >= pos0 + kWeighTiles * 16) continue;
+    if (attend_high(a.s, last) <= pos0 || attend_low(a.s, first) > pos1) continue;
     // the row tiles that see any of these tokens, and the task's share of them
-    const int g_ = a.s.g, end = pos0 + kWeighTiles * 16;
-    const int64_t beyond = a.s.window ? ((int64_t)end + a.s.window - 1 - first) * g_ : w.q.rows;
+    const int g_ = a.s.g;
+    const int64_t beyond = a.s.window ? ((int64_t)pos1 + a.s.window - first) * g_ : w.q.rows;
     const int t0 = pos0 > first ? (int)(((int64_t)pos0 - first) * g_ / 16) : 0, t1 = (int)((min(beyond, (int64_t)w.q.rows) + 15) / 16);
     const int64_t all = max(t1 - t0, 0);
     const int from = t0 + (int)(all * share / g.shares), to = t0 + (int)(all * (share + 1) / g.shares);
@@ -736,7 +736,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
       // a row that is not there, or that sees nothing: no weight, and a reference that no score comes near
       const bool none = t * 16 + col >= w.q.rows || x.end.y == 0.f;
       const float f = none ? 0.f : 1.f / x.end.y, ref = none ? -kNothing : x.end.x;
-      const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) < end || there != (1 << kWeighTiles) - 1;
+      const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) <= pos1 || there != (1 << kWeighTiles) - 1;
       const int low = attend_low(a.s, x.pos);
       const uint32_t span = max(attend_high(a.s, x.pos) - low, 0);
       const bool coarse = uniform(__any(f != 0.f && fabsf(ref) > kCoarse));
@@ -802,46 +802,47 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
 template <bool FEW>
 __global__ __launch_bounds__(kThreads) void weigh_entries_kernel(WeighArgs g) {
   const KvAttendArgs& a = g.a;
-  const int64_t E = a.s.E, at = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3), total = a.s.L * a.s.R * E;
+  const int64_t E = a.s.E, total = a.s.L * a.s.R * E;
   const int part = threadIdx.x & 7;
-  if (at >= total) return;
-  const int e = (int)(at % E);
-  const int64_t lr = at / E;
-  const int r = (int)(lr % a.s.R), l = (int)(lr / a.s.R);
-  const AttendRequest q = request(a, r);
-  float sum = 0.f;
-  if (q.rows) {
-    const int first = q.ctx - q.len, last = first + (q.rows - 1) / a.s.g;
-    const int low = attend_low(a.s, first), high = attend_high(a.s, last);
-    const int id = a.tables[at];
-    const int64_t begin = (int64_t)e * a.s.T;
-    if (id >= 0 && id < a.n_blocks && begin < high && begin + a.s.T > low) {
-      const int per = a.s.T >> 4;
-      if constexpr (FEW) {
-        const int pair = per == 2 ? e : e >> 1;
-        const f32x4* gathered = a.gathered + (lr * a.s.H * (int64_t)a.runs + pair) * a.kept_rows;
-        for (int i = part; i < a.s.H * q.rows; i += 8) {
-          const int h = i / q.rows, n = i - h * q.rows;
-          const f32x4 x = gathered[(int64_t)h * a.runs * a.kept_rows + n];
-          const float2 end = a.ends[row_place<false>(a, l, h, q.first, n)];
-          const float w = per == 2 ? x[0] + x[1] : e & 1 ? x[1] : x[0];
-          const float p = w * __builtin_amdgcn_exp2f(x[2] - end.x) * row_scale(end.y);
-          sum += end.y == 0.f ? 0.f : p;
-        }
-      } else {
-        const float* sums = g.sums + lr * a.s.H * (int64_t)g.tiles + (int64_t)e * per;
-        const int64_t step = a.s.L * a.s.R * a.s.H * (int64_t)g.tiles;
-        for (int i = part; i < a.s.H * g.shares; i += 8) {
-          const int share = i / a.s.H, h = i - share * a.s.H;
-          const float* x = sums + share * step + (int64_t)h * g.tiles;
-          sum += per == 2 ? x[0] + x[1] : x[0];
+  for (int64_t at = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); at < total; at += (int64_t)gridDim.x * 32) {
+    const int e = (int)(at % E);
+    const int64_t lr = at / E;
+    const int r = (int)(lr % a.s.R), l = (int)(lr / a.s.R);
+    const AttendRequest q = request(a, r);
+    float sum = 0.f;
+    if (q.rows) {
+      const int first = q.ctx - q.len, last = first + (q.rows - 1) / a.s.g;
+      const int low = attend_low(a.s, first), high = attend_high(a.s, last);
+      const int id = a.tables[at];
+      const int64_t begin = (int64_t)e * a.s.T;
+      if (id >= 0 && id < a.n_blocks && begin < high && begin + a.s.T > low) {
+        const int per = a.s.T >> 4;
+        if constexpr (FEW) {
+          const int pair = per == 2 ? e : e >> 1;
+          const f32x4* gathered = a.gathered + (lr * a.s.H * (int64_t)a.runs + pair) * a.kept_rows;
+          for (int i = part; i < a.s.H * q.rows; i += 8) {
+            const int h = i / q.rows, n = i - h * q.rows;
+            const f32x4 x = gathered[(int64_t)h * a.runs * a.kept_rows + n];
+            const float2 end = a.ends[row_place<false>(a, l, h, q.first, n)];
+            const float w = per == 2 ? x[0] + x[1] : e & 1 ? x[1] : x[0];
+            const float p = w * __builtin_amdgcn_exp2f(x[2] - end.x) * row_scale(end.y);
+            sum += end.y == 0.f ? 0.f : p;
+          }
+        } else {
+          const float* sums = g.sums + lr * a.s.H * (int64_t)g.tiles + (int64_t)e * per;
+          const int64_t step = a.s.L * a.s.R * a.s.H * (int64_t)g.tiles;
+          for (int i = part; i < a.s.H * g.shares; i += 8) {
+            const int share = i / a.s.H, h = i - share * a.s.H;
+            const float* x = sums + share * step + (int64_t)h * g.tiles;
+            sum += per == 2 ? x[0] + x[1] : x[0];
+          }
         }
       }
     }
-  }
 #pragma unroll
-  for (int d = 4; d; d >>= 1) sum += __shfl_xor(sum, d);
-  if (part == 0) g.out[at] = g.in ? g.in[at] + sum : sum;
+    for (int d = 4; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if (part == 0) g.out[at] = g.in ? g.in[at] + sum : sum;
+  }
 }
 
 // ---- The call.
@@ -869,7 +870,8 @@ struct WeighRoom {
   int64_t bytes() const { return ends + gathered + sums; }
 };
 constexpr int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
-constexpr int kFewRows = 32, kMostShares = 16;
+constexpr int kFewRows = 32, kMostShares = 16, kMostWaves = 4096;
+constexpr int64_t kMostSharedBytes = 2 * kMostWaves * kWeighTiles * 4;
 constexpr int64_t kMostEntries = 1 << 29;  // table entries of a call that weighs them
 
 inline int64_t runs_of(const AttendShape& s) { return ((int64_t)s.cap + 31) / 32; }
@@ -878,7 +880,7 @@ inline WeighRoom many_room(int64_t L, int64_t R, int64_t H, int64_t runs, int64_
   // a few thousand waves, of 8 row tiles at least
   const double chunks = (double)L * R * H * ((runs * 2 + kWeighTiles - 1) / kWeighTiles);
   int64_t shares = 1;
-  while (shares < kMostShares && shares * 2 * 128 <= rows && chunks * shares < 4096) shares *= 2;
+  while (shares < kMostShares && shares * 2 * 128 <= rows && chunks * shares < kMostWaves) shares *= 2;
   return {0, 0, up16(shares * L * R * H * runs * 2 * 4), (int32_t)shares};
 }
 inline WeighRoom weigh_room(const AttendShape& s) {
@@ -942,7 +944,8 @@ void kv_launch(const WeighArgs& g, hipStream_t st) {
     const int64_t tasks = a.s.L * a.s.R * a.s.H * ((g.tiles + kWeighTiles - 1) / kWeighTiles) * (int64_t)g.shares, wgs = (tasks + kWaves - 1) / kWaves;
     weigh_many_kernel<BF16><<<dim3((unsigned)(wgs < (1 << 22) ? wgs : (1 << 22))), kThreads, 0, st>>>(g);
   }
-  const dim3 grid((unsigned)((entries + 31) / 32));
+  const int64_t wgs = (entries + 31) / 32;
+  const dim3 grid((unsigned)(wgs < (1 << 22) ? wgs : (1 << 22)));
   few ? weigh_entries_kernel<true><<<grid, kThreads, 0, st>>>(g) : weigh_entries_kernel<false><<<grid, kThreads, 0, st>>>(g);
 }
 
@@ -967,7 +970,9 @@ extern "C" size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_
   if (weigh && max_q > 0) {
     if ((double)s.L * n_q * n_heads > 1e15) return 0;
     const int64_t runs = runs_of(s), few = max_q < kFewRows / s.g ? max_q : kFewRows / s.g;
-    const int64_t a = few_room(s.L, R, s.H, runs, few * s.g).bytes(), b = kMostShares * many_room(s.L, R, s.H, runs, 1).bytes();
+    // many rows: more shares than one are taken while there are fewer than 8192 waves, of kWeighTiles sums each
+    const int64_t one = many_room(s.L, R, s.H, runs, 1).bytes(), shared = kMostShares * one < kMostSharedBytes ? kMostShares * one : kMostSharedBytes;
+    const int64_t a = few_room(s.L, R, s.H, runs, few * s.g).bytes(), b = one > shared ? one : shared;
     n = (size_t)up16((int64_t)n) + (size_t)up16(s.L * n_q * n_heads * 8) + (size_t)(max_q > kFewRows / s.g && b > a ? b : a);
   }
   return n;

@@ -495,6 +495,28 @@ def test_window_behind_a_short_table(T, E, m, g):
         p.check(r)
 
 
+@pytest.mark.parametrize("m", [1, 40])
+@pytest.mark.parametrize("T,R,E", [(16, 1, (1 << 27) - 5), (32, 1, (1 << 26) - 3), (16, 1 << 10, 1 << 19)])
+def test_largest_tables(T, R, E, m):
+    """The longest tables there are (positions to 2^31 - 64), and 2^29 entries that are weighed: as in a table of the last entries alone, which are all that a window sees."""
+    say(T, R, E, m)
+    gn = gen(R)
+    few = [(int(torch.randint(180, 300, (1,), generator=gn)), int(torch.randint(0, 2, (1,), generator=gn))) for _ in range(R - 1)]
+    p = Problem([(20 * T, m)] + few, 1, 1, T, HALF, E=20)
+    p.window = 100
+    # only requests of one can be as long: many stand at the beginning of their tables
+    at = E - 20 if R == 1 else 0
+    tables = torch.full((1, R, E), -1, dtype=torch.int32, device=DEV)
+    tables[:, :, at:at + 20] = p.tables.to(DEV)
+    # (what this call needs: the size for up to 40 query tokens holds for 32 rows of the other kernels as well)
+    r = p.run(tables=tables, ctx_len=ints([n + at * T for n in p.ctx]), workspace=torch.empty(5 << 30, dtype=torch.uint8, device=DEV))
+    w = r["weights"]
+    r["weights"] = w[:, :, at:at + 20].clone()
+    w[:, :, at:at + 20] = 0
+    assert not w.any()
+    p.check(r)
+
+
 # ---- streams, graphs, workspaces
 
 @pytest.mark.parametrize("m,g", [(1, 5), (3, 8), (15, 4), (40, 3)])
@@ -598,6 +620,22 @@ def test_evict_blocks_that_many_requests_hold():
     refcount.fill_(1000)
     keep = [10] * 50
     check_evict(run_evict(tables, weights, ctx, keep, refcount, 16), ref.evict(tables, weights, ctx, keep, refcount, 16, 1, 1))
+
+
+def test_evict_from_four_million_tables():
+    R, E, T = (1 << 22) + 5, 1025, 16
+    g = gen(8)
+    ids, weights = torch.randint(0, 4000, (3, E), generator=g, dtype=torch.int32), torch.rand((3, E), generator=g)
+    which = torch.arange(R, device=DEV) % 3
+    tables, refcount = ids.to(DEV)[which][None], torch.full((1, 4000), 1 << 30, dtype=torch.int32)
+    ctx, keep = torch.full((R,), E * T, dtype=torch.int32, device=DEV), torch.full((R,), E - 1, dtype=torch.int32, device=DEV)
+    got = rc.rc_kv_evict(tables, weights.to(DEV)[which][None], ctx, keep, refcount.to(DEV), T, in_place=True)
+    want = ref.evict(ids[None], weights[None], [E * T] * 3, [E - 1] * 3, refcount, T, 1, 1)[0]
+    assert (got["n_evicted"] == 1).all()
+    for i in range(3):
+        assert (got["tables"][0, i::3] == want[0, i].to(DEV)).all()
+        refcount[0, ids[i][want[0, i] < 0].item()] -= len(range(i, R, 3))
+    assert torch.equal(got["refcount"].cpu(), refcount)
 
 
 def test_evict_nothing():

@@ -735,8 +735,10 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
       const int p0 = first + t * 16 / g_, p1 = first + min(t * 16 + 15, w.q.rows - 1) / g_;
       // a row that is not there, or that sees nothing: no weight, and a reference that no score comes near
       const bool none = t * 16 + col >= w.q.rows || x.end.y == 0.f;
-      const float f = none ? 0.f : 1.f / x.end.y, ref = none ? -kNothing : x.end.x;
+      // a row that is not finite has a NaN where it sees a token, and only there
+      const bool bad = !none && !(fabsf(x.end.x) < __builtin_inff() && x.end.y < __builtin_inff());
       const bool ends = attend_low(a.s, p1) > pos0 || attend_high(a.s, p0) <= pos1 || there != (1 << kWeighTiles) - 1;
+      const float f = none ? 0.f : bad ? 1.f : 1.f / x.end.y, ref = none ? -kNothing : bad ? ends ? 0.f : __builtin_nanf("") : x.end.x;
       const int low = attend_low(a.s, x.pos);
       const uint32_t span = max(attend_high(a.s, x.pos) - low, 0);
       const bool coarse = uniform(__any(f != 0.f && fabsf(ref) > kCoarse));
@@ -754,7 +756,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
           for (int i = 0; i < 16; ++i) {
             const int j = j0 + (i >> 2);
             const bool is = (uint32_t)(pos0 + 16 * j + 4 * quarter + (i & 3) - low) < (there >> j & 1 ? span : 0u);
-            s[i >> 2][i & 3] = is ? s[i >> 2][i & 3] : -__builtin_inff();
+            s[i >> 2][i & 3] = !is ? -__builtin_inff() : bad ? __builtin_nanf("") : s[i >> 2][i & 3];
           }
         }
         if (__builtin_expect(coarse, 0)) {
@@ -819,9 +821,12 @@ __global__ __launch_bounds__(kThreads) void weigh_entries_kernel(WeighArgs g) {
         const int per = a.s.T >> 4;
         if constexpr (FEW) {
           const int pair = per == 2 ? e : e >> 1;
+          // where some rows do not see the entry: what these left may be a NaN
+          const bool some = begin < attend_low(a.s, last) || begin + a.s.T > attend_high(a.s, first);
           const f32x4* gathered = a.gathered + (lr * a.s.H * (int64_t)a.runs + pair) * a.kept_rows;
           for (int i = part; i < a.s.H * q.rows; i += 8) {
             const int h = i / q.rows, n = i - h * q.rows;
+            if (some && (begin >= attend_high(a.s, first + n / a.s.g) || begin + a.s.T <= attend_low(a.s, first + n / a.s.g))) continue;
             const f32x4 x = gathered[(int64_t)h * a.runs * a.kept_rows + n];
             const float2 end = a.ends[row_place<false>(a, l, h, q.first, n)];
             const float w = per == 2 ? x[0] + x[1] : e & 1 ? x[1] : x[0];

@@ -253,6 +253,23 @@ def test_queries_that_are_not_finite_stay_in_their_rows():
     assert r["out"][0, 0, 1].isnan().all() and r["out"][0, 1, 7].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", [HALF, BF])
+@pytest.mark.parametrize("m,g", [(2, 3), (8, 4), (16, 1), (30, 1), (40, 2), (300, 3)])
+@pytest.mark.parametrize("window", [0, 1, 20, 150])
+def test_rows_that_are_not_finite_weigh_on_what_they_see_alone(m, g, window, dtype):
+    say(m, g, window, dtype)
+    p = Problem([(300, m), (320, m), (310, m)], 2, g, 16, dtype)
+    p.window = window
+    p.q[0, m // 3, 1 % g, 5] = math.nan
+    # a key of the third request that makes a score of infinity for the rows that see it, from the middle of the step on
+    p.q[..., 3] = p.q[..., 3].abs() + 0.25
+    p.k[0, 300 + 320 + 310 - 1 - m // 2, 1, 3] = math.inf
+    p.rewrite()
+    r = p.run()
+    p.check(r)
+    assert not torch.isfinite(r["weights"]).all() and (window == 0 or torch.isfinite(r["weights"]).any())
+
+
 @pytest.mark.parametrize("dtype,spread", [(HALF, 2.0 ** -17), (HALF, 3000.0), (BF, 1e-30), (BF, 1e30), (BF, 2.0 ** -118)])
 @pytest.mark.parametrize("m", [1, 30])
 def test_values_of_any_size(dtype, spread, m):

@@ -732,7 +732,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_many_kernel(WeighArgs g) {
       for (int d = 0; d < 4; ++d) x.q[d] = *(const u32x4*)(p + d * 64);
     };
     const auto add_rows = [&](const Rows& x, int t) RC_INLINE {
-      const int p0 = first + t * 16 / g_, p1 = first + min(t * 16 + 15, w.q.rows - 1) / g_;
+      const int p0 = __builtin_amdgcn_readlane(x.pos, 0), p1 = __builtin_amdgcn_readlane(x.pos, 15);
       // a row that is not there, or that sees nothing: no weight, and a reference that no score comes near
       const bool none = t * 16 + col >= w.q.rows || x.end.y == 0.f;
       // a row that is not finite has a NaN where it sees a token, and only there

@@ -670,8 +670,10 @@ struct WeighArgs {
 
 // Many rows: the probabilities are taken once more, from K, Q and the rows' final references and sums: a wave holds the K of 128 tokens and goes through a
 // share of the rows that see them.  (Kept from the first time they would be a number for each row and 16 tokens: 10 GB for a prompt of 32k tokens and 40 heads.)
-// Prompts of 2500 tokens and 32 heads: 51 GFLOP in 105 us, bound by the way of Q from the caches (117 us where 64 tokens a wave take 142, 32 and 64 shares of the rows
-// instead of 16 122 and 149; with the rows read when they are needed 228, with one tile's products after another's 147).
+// Prompts of 2500 tokens and 32 heads: 51 GFLOP in 103 us at the card's steady speed (115 before it).  What bounds it is what a SIMD issues: a power and its sums take
+// twice the cycles of the products (the matrix units are busy for 19 % of the time).  64 tokens a wave 142 us for 117, 32 and 64 shares of the rows instead of 16 122 and 149;
+// with the rows read when they are needed 228, two tiles ahead 116 for 115, with one tile's products after another's 147, four tiles' products beside the powers of the
+// last four 123 for 115.
 constexpr int kWeighTiles = 8;
 
 template <bool BF16>

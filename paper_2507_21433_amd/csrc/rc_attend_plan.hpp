@@ -1,4 +1,4 @@
-// How the work of rc_cache_attend is cut into equal shares.  Plain C++ (host and device), so that the arithmetic can be checked
+// How the work of rc_cache_attend and rc_kv_attend is cut into equal shares.  Plain C++ (host and device), so that the arithmetic can be checked
 // where there is no GPU.
 //
 // The query tokens of a request times the query heads of one KV head are its rows, in tiles of `rows` rows.  An item is one row
@@ -155,6 +155,22 @@ inline AttendKernel attend_kernel(int64_t rows, double pairs, int64_t steps) {
   const double tiles = pairs * (double)((rows + 127) / 128);
   if (rows <= 64 || (tiles <= 128 && tiles * (double)steps <= 8192)) return {64, 64, 512, 8, 1};
   return {128, 64, 512, 8, 1};
+}
+
+// The same over 16-bit blocks, by the rows of a request and KV head (query tokens times heads of a KV head): tiles of 16 and 32 rows, where every wave of a workgroup has all rows
+// and a quarter of the tokens, and of 64, 128 and 192, where every wave has a quarter of the rows.  Larger tiles read the blocks less often and cost
+// more to begin and end.  us with tiles of 64 / 128 / 192 rows, by the number of tiles of 128 and of steps of 64 tokens that a table has: 8 x 63 23 / 28 / 33,
+// 64 x 16 28 / 37 / 42, 24 x 63 33 / 33 / 39, 32 x 63 32 / 36 / 43, 64 x 63 50 / 52 / 62, 256 x 16 35 / 42 / 43; 320 x 16 53 / 39 / 43,
+// 512 x 8 39 / 34 / 39, 24 x 250 62 / 58 / 70, 128 x 63 71 / 67 / 82, 64 x 250 121 / 105 / 108, 2560 x 5 103 / 82 / 86; 640 x 63 - / 194 / 200,
+// 320 x 125 - / 195 / 193, 260 x 250 - / 361 / 336, 1280 x 125 - / 671 / 632.  An item of many rows costs three steps besides its own (1, 3 and 5 tried:
+// prompts of 2500 tokens 181, 152 and 154 us, a chunk of 1024 285 to 289).
+inline AttendKernel kv_kernel(int64_t rows, double pairs, int64_t steps) {
+  if (rows <= 16) return {16, 128, 768, 4, 2};
+  if (rows <= 32) return {32, 128, 512, 4, 1};
+  const double tiles = pairs * (double)((rows + 127) / 128), work = tiles * (double)steps;
+  if (rows <= 64 || (tiles <= 256 && work <= 4096)) return {64, 64, 512, 8, 1};
+  if (work <= 49152) return {128, 64, 512, 8, 3};
+  return {192, 64, 512, 8, 3};
 }
 
 // Most units of an item, whatever the lengths.

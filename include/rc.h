@@ -550,7 +550,8 @@ size_t rc_kv_attend_workspace_size(const rc_kv_desc* desc, int64_t n_blocks, int
  * at most 32, else one.  No atomics: the same bits on every run.  Sums of finite values neither overflow nor lose their values (but weights are not
  * defined where scale * log2(e) * q.k is beyond 2^20, so that fp32 numbers there are whole ones, and bf16 values are beyond 2^64 at the same time); a query
  * that sees an infinity or a NaN in V has infinities or NaNs in these dims, one that does not see them is as if they were not there.  A query with a
- * score of infinity or NaN leaves a NaN in the weights of the entries that it sees, and in no others.
+ * score of plus infinity or NaN leaves a NaN in the weights of the entries that it sees, and in no others.  A token scored minus infinity has a probability
+ * of 0, and a query all of whose scores are that is one that sees nothing.
  */
 rc_status rc_kv_attend(const rc_kv_desc* desc, int64_t n_blocks, const void* k, const void* v, const int32_t* tables, int64_t R, int64_t E,
                        const int32_t* ctx_len, const int32_t* q_start, const void* q, int64_t n_q, int32_t n_heads,

@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void attend_rows_kernel(
       return;
     }
     if (w.item.pairs == 0) {
-      store_nothing<true>(a, w);
+      store_nothing<true, false>(a, w);
       if (!go_on<true>(a, wg, w, part)) return;
       continue;
     }
@@ -374,7 +374,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_many_kernel(CacheAttendArg
       return;
     }
     if (w.item.pairs == 0) {
-      store_nothing<false>(a, w);
+      store_nothing<false, false>(a, w);
       if (!go_on<false>(a, wg, w, cut)) return;
       continue;
     }

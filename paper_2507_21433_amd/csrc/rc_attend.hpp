@@ -364,15 +364,16 @@ __device__ __forceinline__ void load_q(const AttendArgs& a, const Walk& w, int n
   for (int s = 0; s < 4; ++s) q[s] = p[s];
 }
 
-// The rows of an item that sees nothing.
-template <bool ONE>
+// The rows of an item that sees nothing.  ENDS: a.ends may be there.  (Known when compiled: asked of a.ends alone, it costs the attention over the 4-bit
+// cache scalar registers that it does not have, and 64 decoding requests of 12400 tokens take 115.6 us instead of 111.6.)
+template <bool ONE, bool ENDS>
 __device__ inline void store_nothing(const AttendArgs& a, const Walk& w) {
   const int rows = min(a.s.rows, w.q.rows - w.t * a.s.rows);
   for (int i = threadIdx.x; i < rows * 16; i += kThreads) {
     const int64_t at = row_place<ONE>(a, w, w.t * a.s.rows + (i >> 4));
     *(u32x4*)(a.out + (at * 128 + (i & 15) * 8) * 2) = u32x4{0, 0, 0, 0};
     if ((i & 15) == 0 && a.lse) a.lse[at] = -__builtin_inff();
-    if ((i & 15) == 0 && a.ends) a.ends[at] = float2{kNothing, 0.f};
+    if (ENDS && (i & 15) == 0 && a.ends) a.ends[at] = float2{kNothing, 0.f};
   }
 }
 

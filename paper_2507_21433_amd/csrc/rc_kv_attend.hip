@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
       return;
     }
     if (w.item.pairs == 0) {
-      store_nothing<true>(a, w);
+      store_nothing<true, true>(a, w);
       if (!go_on<true>(a, wg, w, part)) return;
       continue;
     }
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(KvAttendArgs a) {
       return;
     }
     if (w.item.pairs == 0) {
-      store_nothing<false>(a, w);
+      store_nothing<false, true>(a, w);
       if (!go_on<false>(a, wg, w, cut)) return;
       continue;
     }

@@ -182,9 +182,16 @@ def _kv_pair(k, v, alike=False):
     return shape, d
 
 
+# The library launches on the current device and its stream, where memory of another device may not be mapped.
 def _dev(*ts):
+    at = None
     for t in ts:
-        assert t is None or t.is_cuda, "device tensors only"
+        if t is not None:
+            d = t.get_device()
+            if d != at:
+                assert at is None and d >= 0, "device tensors only, all of one device"
+                at = d
+    assert at is None or at == torch._C._cuda_getDevice(), "tensors of the current device only"
 
 
 def rc_block_norms(k, v, mode=RC_SCORE_BLOCK, k_sqnorm=None, v_sqnorm=None):

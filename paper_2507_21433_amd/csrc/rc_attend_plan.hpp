@@ -163,7 +163,8 @@ inline AttendKernel attend_kernel(int64_t rows, double pairs, int64_t steps) {
 // 64 x 16 28 / 37 / 42, 24 x 63 33 / 33 / 39, 32 x 63 32 / 36 / 43, 64 x 63 50 / 52 / 62, 256 x 16 35 / 42 / 43; 320 x 16 53 / 39 / 43,
 // 512 x 8 39 / 34 / 39, 24 x 250 62 / 58 / 70, 128 x 63 71 / 67 / 82, 64 x 250 121 / 105 / 108, 2560 x 5 103 / 82 / 86; 640 x 63 - / 194 / 200,
 // 320 x 125 - / 195 / 193, 260 x 250 - / 361 / 336, 1280 x 125 - / 671 / 632.  An item of many rows costs three steps besides its own (1, 3 and 5 tried:
-// prompts of 2500 tokens 181, 152 and 154 us, a chunk of 1024 285 to 289).
+// prompts of 2500 tokens 181, 152 and 154 us, a chunk of 1024 285 to 289).  Steps are those of the tables' width: 384 query tokens over 4000 take 31 us in tables of
+// that width and 41 in tables for 131072 positions, two requests of 256 over 2000 34 and 56.
 inline AttendKernel kv_kernel(int64_t rows, double pairs, int64_t steps) {
   if (rows <= 16) return {16, 128, 768, 4, 2};
   if (rows <= 32) return {32, 128, 512, 4, 1};

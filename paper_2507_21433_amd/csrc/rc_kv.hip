@@ -75,9 +75,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // i * threads + thread at place i), so that a count is a compare and a ballot for each; a row that they do not hold is counted by a histogram of
 // each byte in turn, for which it is read again.
 //
-// 64 layers of 64 requests of up to 775 entries, 700 kept at most: 29 us and 5 for the copy of the reference counts; 11 of these are the 1M decrements, 11 the tables and
-// weights going in and out, the borders the rest (a histogram by bytes for these as well: the same).  24 tables of 16384 entries cut down to a quarter: 46 us, 24 workgroups'
-// work, 19 for the decrements (with histograms 62).
+// 64 layers of 64 requests of up to 775 entries, 700 kept at most: 27 us and 5 for the copy of the reference counts; 11 of these are the 0.43M decrements, 11 the tables and
+// weights going in and out, the borders the rest (a histogram by bytes for these as well: the same).  24 tables of 16384 entries cut down to a quarter: 45 us, 24 workgroups'
+// work, 19 for the 0.22M decrements (with histograms 62).
 template <int WAVES, int ITEMS>  // ITEMS: entries of a thread held in registers, 0: none
 struct EvictRow {
   static constexpr int kRowThreads = 64 * WAVES;

@@ -164,8 +164,9 @@ struct RowsLds {
 // waves.  With weights a wave leaves the sums of the two tiles of a run and its reference for every row, 16 bytes beside the run's 16384.
 template <bool BF16, int RT, bool STREAM, bool WEIGH>
 __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
-  // Probabilities are sums of two 16-bit numbers: the matrix cores have the time (24 rows over 305 MB: 72 us, and 84 with
-  // one number, where the compiler spills 328 B a thread instead of 184), and the only rounding that counts is that of the output.
+  // Probabilities are sums of two 16-bit numbers: the matrix cores have the time, and the only rounding that counts is that of the output.  24 rows over
+  // 305 MB, two numbers and one: bf16 78 and 89 us (184 and 328 B a thread in memory), fp16 90 and 90 (336 B either way); with weights 102 and 111 in
+  // both types (188 and 340).  Against 64 bits the outputs of one number are 1.3 times as far off.
   __shared__ RowsLds<RT> lds;
   const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), quarter = lane >> 4, col = lane & 15;
   const int wg = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_rows_kernel(KvAttendArgs a) {
 //
 // A run of a wave with 48 rows is 48 matrix instructions (768 cycles), some 110 other vector instructions, 24 of them exponentials, and 16 KB of LDS.  A chunk of
 // 1024 query tokens over 8192: 220 GFLOP in 237 us at the card's steady speed (930 TFLOP/s; a library product of 8192^3 runs at 1155) and 16 for the parts of cut items; a
-// SIMD's matrix unit is busy for 39 % of the time, its other vector instructions take 28 %, a compute unit's LDS 20 %.  Two waves a SIMD, each a chain of reads, products, exponentials and products, do not cover each other's waits:
+// SIMD's matrix unit is busy for 39 % of the time, its other vector instructions take 28 % at four cycles each and more where they are exponentials, a compute unit's LDS 20 %.  Two waves a SIMD, each a chain of reads, products, exponentials and products, do not cover each other's waits:
 // workgroups of equal work end between 190 and 286 us.  What was tried against that (us before the card has reached its speed, 256 as it is): wave tiles of 32 rows 280 us, steps of 64 tokens to a barrier 258, products
 // woven between exponentials 260, K and V through registers 293, two groups of four waves that take turns at the matrix cores with a barrier at each turn 320 to 385.
 // Without the loads it takes 8 % less, without the exponentials 14 %.
@@ -560,6 +561,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(KvAttendArgs a) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) rescale<BF16>(s[t], o[t], ref[t], sum[t], top[t], a.c, t, gate, lds.ref[wave][16 * t + col]);
       }
+      // A probability is rounded once to the 16-bit type, as an operand of the second product (the sums of weights take it in fp32).  As the sum of two
+      // such numbers it takes half of this loop's matrix instructions again: the chunk of 1024 336 us for 254, prompts of 2500 tokens 191 for 153, for outputs that are
+      // off by 6.2e-6 instead of 8.6e-6 in the mean square of the chunk (fp16; bf16 4.9e-5 and 6.8e-5), where the rounding of the output itself is most of the former.
       u32x4 v[2][4], p16[RT];
       const auto read_v = [&](int i) RC_INLINE {  // chunks 4 i to 4 i + 3
 #pragma unroll
@@ -670,8 +674,9 @@ struct WeighArgs {
 
 // Many rows: the probabilities are taken once more, from K, Q and the rows' final references and sums: a wave holds the K of 128 tokens and goes through a
 // share of the rows that see them.  (Kept from the first time they would be a number for each row and 16 tokens: 10 GB for a prompt of 32k tokens and 40 heads.)
-// Prompts of 2500 tokens and 32 heads: 51 GFLOP in 103 us at the card's steady speed (115 before it).  What bounds it is what a SIMD issues: a power and its sums take
-// twice the cycles of the products (the matrix units are busy for 19 % of the time).  64 tokens a wave 142 us for 117, 32 and 64 shares of the rows instead of 16 122 and 149;
+// Prompts of 2500 tokens and 32 heads: 51 GFLOP in 103 us at the card's steady speed (115 before it).  Nothing is busy all the time: the matrix units are for 19 % of it, other
+// vector instructions take 31 % at four cycles each, and more where they are exponentials.  Without the loads of rows, which every wave takes from the L2 for itself,
+// a pass takes 18 us less, without the exponentials 8.  64 tokens a wave 142 us for 117, 32 and 64 shares of the rows instead of 16 122 and 149;
 // with the rows read when they are needed 228, two tiles ahead 116 for 115, with one tile's products after another's 147, four tiles' products beside the powers of the
 // last four 123 for 115.
 constexpr int kWeighTiles = 8;
@@ -868,7 +873,8 @@ constexpr int64_t kMostEntries = 1 << 29;  // table entries of a call that weigh
 inline int64_t runs_of(const AttendShape& s) { return ((int64_t)s.cap + 31) / 32; }
 inline WeighRoom few_room(int64_t L, int64_t R, int64_t H, int64_t runs, int64_t rows) { return {0, L * R * H * runs * rows * 16, 0, 0}; }
 inline WeighRoom many_room(int64_t L, int64_t R, int64_t H, int64_t runs, int64_t rows) {
-  // a few thousand waves, of 8 row tiles at least
+  // A few thousand waves, of 8 row tiles at least.  (By the tables' width: those of contexts that fill a small part of their table are fewer.  Prompts of 2500 tokens
+  // in tables for 131072 have one share instead of 16, and their weights take 994 us instead of 103.)
   const double chunks = (double)L * R * H * ((runs * 2 + kWeighTiles - 1) / kWeighTiles);
   int64_t shares = 1;
   while (shares < kMostShares && shares * 2 * 128 <= rows && chunks * shares < kMostWaves) shares *= 2;

@@ -71,8 +71,8 @@ def _kernels_per_call(events, times):
 
 def kernel_names(call):
     """Names of the kernels that call() launches, [] where no kernel trace is to be had.  The profiler can lose events: all of them in a trace of a
-    few microseconds, or one kernel's in all calls.  Of 300 traces of the tests of dispatch 11
-    were cut short in one of these ways.  So a trace is taken again until two whole ones in a row say the same."""
+    few microseconds, or one kernel's in all calls (11 traces of a run of 266 tests of dispatch were cut short).  So a trace is taken again until
+    two whole ones in a row say the same."""
     from torch.profiler import ProfilerActivity, profile
     last = None
     for times in (3, 3, 12, 12, 3, 3, 12, 12, 48, 48):
